@@ -68,6 +68,7 @@ typedef enum owl_dtype {
 #define OWL_DEV_BAD_NDRAFT 16u  /* some n_draft_seq[b] not in [0, n_draft]        */
 #define OWL_DEV_BAD_TOKEN 32u   /* drafter cell: some tokens[r] not in [0, vocab)  */
 #define OWL_DEV_BAD_ROW 64u     /* drafter cell: some parent_row[r] not in [0, n_states) */
+#define OWL_DEV_BAD_LOGIT 128u  /* token log probabilities: some row has a logit that is +infinity or no number */
 
 /*
  * Shape of one verify step.  Strides are in ELEMENTS of qkv_dtype.
@@ -315,6 +316,151 @@ owl_status owl_accept_greedy(const int32_t *tokens, const int32_t *tree_parent, 
 owl_status owl_commit_kv(const owl_verify_desc *desc, void *k_cache, void *v_cache, const int32_t *page_table,
                          const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
                          int32_t *new_ctx_lens, uint32_t *dev_status, void *stream);
+
+/*
+ * Appending new tokens' keys and values to the paged cache, rotary position
+ * embedding on the way: the rows that owl_verify_attn finds at positions
+ * ctx_lens[b] .. are what this call puts there.  For every sequence b and new
+ * token i < n_tokens, with position id t = pos_ids[b][i] (ctx_lens[b] + i if
+ * pos_ids is NULL; owl_prepare_spec_tree gives those of a tree):
+ *     K cache at logical position ctx_lens[b] + i  =  rotate(k_new[b][i], t)
+ *     V cache at logical position ctx_lens[b] + i  =  v_new[b][i]
+ *     q_out[b][i]                                  =  rotate(q[b][i], t)
+ * rotate turns the first rot_dim channels of a head in pairs: with
+ * a = t * inv_freq[f], f < rot_dim / 2, and (x, y) channels f and f + rot_dim/2
+ * (OWL_ROT_HALVES) or 2f and 2f + 1 (OWL_ROT_PAIRS),
+ *     (x, y) -> rot_scale * (x cos a - y sin a, y cos a + x sin a) ,
+ * all of it in 64 bits and rounded once to qkv_dtype, so that far positions
+ * are as exact as near ones; the other channels are copied.
+ *
+ *   desc        batch, head counts, head_dim, paging, strides, max_ctx_len and
+ *               qkv_dtype are used (any owl_dtype); n_draft is not
+ *   n_tokens    >= 1, a drafted tree or a prompt of any length
+ *   q, k_new, v_new   [B][n_tokens] tokens of [heads][D], contiguous channels
+ *               and heads; *_stride elements from one token to the next (so the
+ *               three may be parts of one fused projection); q may be NULL
+ *   inv_freq    [rot_dim / 2] float32, may be NULL if rot_dim is 0
+ *   q_out       [B][n_tokens][Hq][D] contiguous; may be q itself if q_stride is
+ *               Hq * D; NULL iff q is NULL
+ *   page_table  as owl_verify_attn; NULL only if batch is 1; unless n_new_seq is
+ *               given it has to cover max_ctx_len + n_tokens positions
+ *   n_new_seq   optional [B]: sequence b has n_new_seq[b] <= n_tokens new tokens;
+ *               the others' rows are neither read nor written
+ * rot_dim is a multiple of 16, at most D.  Pointers and byte strides are
+ * multiples of 16.  q_out and the caches overlap nothing else; a page under a
+ * new row belongs to one sequence.  Nothing but the new rows is written: a row
+ * whose page-table entry is outside the pool is dropped (OWL_DEV_BAD_PAGE), and so are
+ * all of a sequence whose length is outside [0, max_ctx_len]
+ * (OWL_DEV_BAD_CTX_LEN); n_new_seq[b] is forced into [0, n_tokens]
+ * (OWL_DEV_BAD_NDRAFT).  q_out is written all the same.
+ */
+#define OWL_ROT_HALVES 0
+#define OWL_ROT_PAIRS 1
+typedef struct owl_append_desc {
+    int32_t n_tokens;                       /* new tokens per sequence                      */
+    int32_t rot_dim;                        /* channels of a head that are turned, 0 = none */
+    int32_t rot_style;                      /* OWL_ROT_HALVES or OWL_ROT_PAIRS              */
+    float rot_scale;                        /* multiplies the turned channels, usually 1    */
+    int64_t q_stride, k_stride, v_stride;   /* elements between tokens                      */
+} owl_append_desc;
+
+owl_status owl_append_kv(const owl_verify_desc *desc, const owl_append_desc *append, const void *q, const void *k_new,
+                         const void *v_new, const float *inv_freq, const int32_t *pos_ids, void *q_out,
+                         void *k_cache, void *v_cache, const int32_t *page_table, const int32_t *ctx_lens,
+                         const int32_t *n_new_seq, uint32_t *dev_status, void *stream);
+
+/*
+ * Caches of 8-bit blocks.  A block is what a page holds of one KV head, of K or
+ * of V: 16 tokens of D e4m3 bytes (four exponent and three mantissa bits, bias 7, greatest number 448,
+ * no infinities, 0x7F and 0xFF no number) and one scale byte s, k_scale[page][kv head] or v_scale[page][kv head]
+ * (uint8, contiguous, n_pool_pages * Hkv of them).  A cached number is
+ *     e4m3(byte) * 2^(s - 127) ,   1 <= s <= 254,
+ * in qkv_dtype, which is OWL_BF16 or OWL_F16 here.  In a descriptor for such a
+ * cache the kv strides count bytes, and are multiples of 16.  Half the memory and
+ * traffic of a 16-bit cache.  The calls that write a block choose its scale from
+ * all rows that count in it, as
+ *     the least e >= e0 with  max |number| <= 448 * 2^e ,    s = e + 127 ,
+ * e0 = -117 (OWL_BF16) or -15 (OWL_F16), and round to nearest even.  Powers of
+ * two make it harmless to choose anew: numbers that are in the block
+ * already stay exactly as they are, unless they sink below 2^-6 * 2^e.  Before that, numbers beyond
+ * 1.875 * 2^127 (OWL_BF16) or 1.875 * 2^15 (OWL_F16), the greatest of a block that the
+ * type still holds, become that; one that is infinite or no number becomes no number and does not
+ * count for the scale.
+ *
+ * owl_append_kv_quant: owl_append_kv into such a cache.  The rows that
+ * owl_append_kv would store are what is rounded to 8 bits.  In the block that
+ * holds position ctx_lens[b] the rows before it count for the scale and are kept, rows
+ * behind the last new one are not touched and do not count.
+ */
+owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_desc *append, const void *q,
+                               const void *k_new, const void *v_new, const float *inv_freq, const int32_t *pos_ids,
+                               void *q_out, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                               const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq,
+                               uint32_t *dev_status, void *stream);
+
+/*
+ * owl_verify_attn over a cache of 8-bit blocks; q in desc->qkv_dtype, which is
+ * OWL_BF16 or OWL_F16.  The arithmetic is that of owl_verify_attn on a 16-bit
+ * cache that holds the same numbers.  n_draft_seq as in owl_verify_attn_ragged, or NULL.
+ * The workspace is that of owl_verify_attn_quant_workspace_size, 256-byte
+ * aligned.  owl_verify_attn_quant_init does what owl_verify_attn_init does,
+ * for this call.
+ */
+owl_status owl_verify_attn_quant(const owl_verify_desc *desc, const void *q, const void *k_cache, const void *v_cache,
+                                 const uint8_t *k_scale, const uint8_t *v_scale, const int32_t *page_table,
+                                 const int32_t *ctx_lens, const int32_t *tree_parent, const int32_t *n_draft_seq,
+                                 void *out, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream);
+owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, size_t *bytes);
+owl_status owl_verify_attn_quant_init(const owl_verify_desc *desc);
+
+/*
+ * owl_commit_kv in a cache of 8-bit blocks.  A block that receives a row from
+ * another place gets a new scale, from its rows before ctx_lens[b] + n_accept[b];
+ * the rows behind those are not touched.  Blocks that receive none stay as they are.
+ * All else as owl_commit_kv.
+ */
+owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void *v_cache, uint8_t *k_scale,
+                               uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,
+                               const int32_t *accepted, const int32_t *n_accept, int32_t *new_ctx_lens,
+                               uint32_t *dev_status, void *stream);
+
+/*
+ * What a row of logits says about its tokens (Sec. 2: the target's own next
+ * tokens are what drafts are checked against; Sec. 3.2.1: a node's likeliest
+ * tokens become its children).  For every row r, with x = scale * logits[r],
+ * m = max x and l = sum over the vocabulary of e^(x - m):
+ *     logprob[r][j]       x[t] - m - ln l,  t = tokens[r][j], j < n_given
+ *     entropy[r]          ln l - (sum of (x - m) e^(x - m)) / l
+ *     top_ids[r][j]       the token with the j-th greatest logit, j < n_top,
+ *                         the smaller index first among equals
+ *     top_logprobs[r][j]  its log probability
+ * With n_top = 1 top_ids is target_next (or target_root) of owl_accept_greedy.
+ * A logit of -infinity excludes its token: log probability -infinity, never
+ * among the top; places that are left over hold -1 and -infinity.  A row of nothing else
+ * has entropy 0.  A row with +infinity or no number in it comes out as no
+ * number, with ids -1 (OWL_DEV_BAD_LOGIT).  A given token of -1 stands for none
+ * and has log probability 0; any other outside [0, vocab) has no number (OWL_DEV_BAD_TOKEN).
+ *
+ *   logits        [rows][vocab] in dtype (any owl_dtype), row_stride elements
+ *                 from row to row; any alignment that dtype has
+ *   tokens        [rows][n_given] int32; NULL iff n_given is 0 (0 .. 64)
+ *   logprob       [rows][n_given], entropy [rows] (or NULL), top_ids and
+ *                 top_logprobs [rows][n_top] (each or NULL), n_top 0 .. 32
+ *   workspace     >= owl_token_logprobs_workspace_size() bytes, 256-byte aligned
+ * Sums are formed in float32, in an order that depends on the shape only.
+ */
+typedef struct owl_logprob_desc {
+    int32_t rows, vocab;      /* >= 1                                       */
+    int32_t n_given, n_top;
+    int32_t dtype;            /* owl_dtype of the logits                    */
+    float scale;              /* one over the temperature; finite, positive */
+    int64_t row_stride;       /* elements, >= vocab                         */
+} owl_logprob_desc;
+
+owl_status owl_token_logprobs_workspace_size(const owl_logprob_desc *desc, size_t *bytes);
+owl_status owl_token_logprobs(const owl_logprob_desc *desc, const void *logits, const int32_t *tokens, float *logprob,
+                              float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace,
+                              size_t workspace_bytes, uint32_t *dev_status, void *stream);
 
 /*
  * One step of the drafter's recurrent cell (Sec. 3.2.1, Eq. 1-8): from the token

@@ -21,9 +21,10 @@ OWL_ERR_INVALID_ARG, OWL_ERR_BAD_TREE, OWL_ERR_TOO_MANY_DRAFT = -1, -2, -3
 OWL_ERR_UNSUPPORTED, OWL_ERR_WORKSPACE, OWL_ERR_HIP = -4, -5, -6
 OWL_DEV_BAD_PARENT, OWL_DEV_BAD_PAGE, OWL_DEV_BAD_CTX_LEN, OWL_DEV_BAD_ACCEPT = 1, 2, 4, 8
 OWL_DEV_BAD_NDRAFT = 16
-OWL_DEV_BAD_TOKEN, OWL_DEV_BAD_ROW = 32, 64
+OWL_DEV_BAD_TOKEN, OWL_DEV_BAD_ROW, OWL_DEV_BAD_LOGIT = 32, 64, 128
 OWL_DRAFTER_PROJ, OWL_DRAFTER_GATES, OWL_DRAFTER_ALL = 1, 2, 3
 OWL_W_ROWS, OWL_W_TILED = 0, 1
+OWL_ROT_HALVES, OWL_ROT_PAIRS = 0, 1
 
 OWL_FLAG_FP32_PARTIALS = 1
 
@@ -36,6 +37,8 @@ EXPORTS = (
     "owl_drafter_cell", "owl_drafter_cell_phases", "owl_drafter_cell_workspace_size", "owl_drafter_alpha",
     "owl_drafter_tiled_weight_bytes", "owl_drafter_tile_weights",
     "owl_verify_attn_init", "owl_verify_attn_noalloc",
+    "owl_append_kv", "owl_append_kv_quant", "owl_verify_attn_quant", "owl_verify_attn_quant_workspace_size",
+    "owl_verify_attn_quant_init", "owl_commit_kv_quant", "owl_token_logprobs", "owl_token_logprobs_workspace_size",
     "owl_status_str", "owl_version",
 )
 # ... and in include/owl_probe.h (measurement and self-test aids)
@@ -84,6 +87,22 @@ class DrafterDesc(ctypes.Structure):
         ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
         ("alpha", ctypes.c_float), ("eps", ctypes.c_float),
         ("w_layout", ctypes.c_int32), ("reserved_", ctypes.c_int32),
+    ]
+
+
+class AppendDesc(ctypes.Structure):
+    """Mirror of owl_append_desc."""
+    _fields_ = [
+        ("n_tokens", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("rot_style", ctypes.c_int32), ("rot_scale", ctypes.c_float),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+    ]
+
+
+class LogprobDesc(ctypes.Structure):
+    """Mirror of owl_logprob_desc."""
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("n_given", ctypes.c_int32), ("n_top", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("row_stride", ctypes.c_int64),
     ]
 
 
@@ -171,6 +190,22 @@ def lib() -> ctypes.CDLL:
         l.owl_accept_greedy.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
         l.owl_commit_kv.restype = ctypes.c_int
         l.owl_commit_kv.argtypes = [ctypes.POINTER(VerifyDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        l.owl_append_kv.restype = ctypes.c_int
+        l.owl_append_kv.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(AppendDesc)] + [vp] * 13
+        l.owl_append_kv_quant.restype = ctypes.c_int
+        l.owl_append_kv_quant.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(AppendDesc)] + [vp] * 15
+        l.owl_verify_attn_quant.restype = ctypes.c_int
+        l.owl_verify_attn_quant.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11 + [ctypes.c_size_t, vp, vp]
+        l.owl_verify_attn_quant_workspace_size.restype = ctypes.c_int
+        l.owl_verify_attn_quant_workspace_size.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(ctypes.c_size_t)]
+        l.owl_verify_attn_quant_init.restype = ctypes.c_int
+        l.owl_verify_attn_quant_init.argtypes = [ctypes.POINTER(VerifyDesc)]
+        l.owl_commit_kv_quant.restype = ctypes.c_int
+        l.owl_commit_kv_quant.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11
+        l.owl_token_logprobs.restype = ctypes.c_int
+        l.owl_token_logprobs.argtypes = [ctypes.POINTER(LogprobDesc)] + [vp] * 7 + [ctypes.c_size_t, vp, vp]
+        l.owl_token_logprobs_workspace_size.restype = ctypes.c_int
+        l.owl_token_logprobs_workspace_size.argtypes = [ctypes.POINTER(LogprobDesc), ctypes.POINTER(ctypes.c_size_t)]
         l.owl_status_str.restype = ctypes.c_char_p
         l.owl_status_str.argtypes = [ctypes.c_int]
         l.owl_version.restype = ctypes.c_char_p
@@ -419,6 +454,66 @@ def owl_verify_attn_ragged(desc: VerifyDesc, q, k_cache, v_cache, page_table, ct
                                       _ptr(workspace), workspace.numel() * workspace.element_size(),
                                       _ptr(dev_status), _stream() if stream is None else stream)
     _check(rc, "owl_verify_attn_ragged")
+
+
+def owl_append_kv(desc: VerifyDesc, append: AppendDesc, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, page_table,
+                  ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
+    """q, k_new, v_new may be views of one fused projection: only their first elements and ``append``'s strides count."""
+    rc = lib().owl_append_kv(ctypes.byref(desc), ctypes.byref(append), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(inv_freq),
+                             _ptr(pos_ids), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(ctx_lens),
+                             _ptr(n_new_seq), _ptr(dev_status), _stream() if stream is None else stream)
+    _check(rc, "owl_append_kv")
+
+
+def owl_append_kv_quant(desc: VerifyDesc, append: AppendDesc, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale,
+                        v_scale, page_table, ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
+    rc = lib().owl_append_kv_quant(ctypes.byref(desc), ctypes.byref(append), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(inv_freq),
+                                   _ptr(pos_ids), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
+                                   _ptr(page_table), _ptr(ctx_lens), _ptr(n_new_seq), _ptr(dev_status),
+                                   _stream() if stream is None else stream)
+    _check(rc, "owl_append_kv_quant")
+
+
+def owl_verify_attn_quant_workspace_size(desc: VerifyDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().owl_verify_attn_quant_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "owl_verify_attn_quant_workspace_size")
+    return int(n.value)
+
+
+def owl_verify_attn_quant_init(desc: VerifyDesc) -> None:
+    _check(lib().owl_verify_attn_quant_init(ctypes.byref(desc)), "owl_verify_attn_quant_init")
+
+
+def owl_verify_attn_quant(desc: VerifyDesc, q, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, tree_parent, n_draft_seq,
+                          out, workspace, dev_status=None, stream: Optional[int] = None) -> None:
+    """owl_verify_attn over a cache of 8-bit blocks: uint8 (or float8_e4m3fn) pools, uint8 scales [n_pool_pages][Hkv]."""
+    rc = lib().owl_verify_attn_quant(
+        ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(page_table), _ptr(ctx_lens),
+        _ptr(tree_parent), _ptr(n_draft_seq), _ptr(out), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+        _ptr(dev_status), _stream() if stream is None else stream)
+    _check(rc, "owl_verify_attn_quant")
+
+
+def owl_commit_kv_quant(desc: VerifyDesc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,
+                        new_ctx_lens=None, dev_status=None, stream: Optional[int] = None) -> None:
+    rc = lib().owl_commit_kv_quant(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(page_table),
+                                   _ptr(ctx_lens), _ptr(accepted), _ptr(n_accept), _ptr(new_ctx_lens), _ptr(dev_status),
+                                   _stream() if stream is None else stream)
+    _check(rc, "owl_commit_kv_quant")
+
+
+def owl_token_logprobs_workspace_size(desc: LogprobDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().owl_token_logprobs_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "owl_token_logprobs_workspace_size")
+    return int(n.value)
+
+
+def owl_token_logprobs(desc: LogprobDesc, logits, tokens, logprob, entropy, top_ids, top_logprobs, workspace, dev_status=None,
+                       stream: Optional[int] = None) -> None:
+    rc = lib().owl_token_logprobs(ctypes.byref(desc), _ptr(logits), _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(top_ids),
+                                  _ptr(top_logprobs), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
+                                  _ptr(dev_status), _stream() if stream is None else stream)
+    _check(rc, "owl_token_logprobs")
 
 
 def owl_mfma_probe(src, iters: int, sink, n_workgroups: int, stream: Optional[int] = None, clock_ghz=None) -> None:

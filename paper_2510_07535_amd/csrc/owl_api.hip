@@ -69,9 +69,20 @@ struct FullPlan {
     dim3 grid;                // of the split-KV pass
 };
 
-owl_status make_plan(const owl_verify_desc *d, FullPlan *fp)
+// What a descriptor for a cache of 8-bit blocks has to be beyond that: its kv strides count bytes.
+owl_status check_quant_desc(const owl_verify_desc *d)
 {
     owl_status st = check_desc(d);
+    if (st != OWL_OK) return st;
+    if (d->qkv_dtype == OWL_F32) return OWL_ERR_UNSUPPORTED;
+    for (int64_t s : {d->kv_stride_page, d->kv_stride_head, d->kv_stride_token})
+        if (s % 16 != 0) return OWL_ERR_INVALID_ARG;
+    return OWL_OK;
+}
+
+owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
+{
+    owl_status st = quant ? check_quant_desc(d) : check_desc(d);
     if (st != OWL_OK) return st;
     const int G = d->n_q_heads / d->n_kv_heads;
     const int R = G * d->n_draft;
@@ -159,7 +170,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp)
         else if (caps[li] == 8 && group_tiles >= 7 && piece >= 32 && share >= (group_tiles == 8 ? 64 : 256)) { tpw = 2; wr = 4; wk = 2; }
         else { wr = 8; wk = 1; tpw = (group_tiles + 7) / 8; }
     }
-    const Variant *v = find_variant(d->qkv_dtype, d->head_dim, tpw, wr, wk);
+    const Variant *v = find_variant(d->qkv_dtype, d->head_dim, tpw, wr, wk, false, quant);
     if (!v) return OWL_ERR_UNSUPPORTED;
     fp->group_tiles = group_tiles;
     int64_t C;
@@ -323,6 +334,8 @@ owl_status scratch_address(void **out)
     return OWL_OK;
 }
 
+constexpr int kMaxGrid = 65535;                 // workgroups along the second and third dimension of a grid
+
 bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
 
 }  // namespace
@@ -363,7 +376,8 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
                               const void *v_cache, const int32_t *page_table, const int32_t *ctx_lens,
                               const int32_t *tree_parent, const int32_t *n_draft_seq, void *out,
                               void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream,
-                              int32_t phases, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr);
+                              int32_t phases, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr,
+                              const uint8_t *k_scale = nullptr, const uint8_t *v_scale = nullptr);
 
 owl_status owl_verify_attn_phases(const owl_verify_desc *desc, const void *q, const void *k_cache,
                                   const void *v_cache, const int32_t *page_table,
@@ -390,11 +404,13 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
                               const void *v_cache, const int32_t *page_table, const int32_t *ctx_lens,
                               const int32_t *tree_parent, const int32_t *n_draft_seq, void *out,
                               void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream,
-                              int32_t phases, hipEvent_t ev_start, hipEvent_t ev_stop)
+                              int32_t phases, hipEvent_t ev_start, hipEvent_t ev_stop, const uint8_t *k_scale,
+                              const uint8_t *v_scale)
 {
     if (phases < 1 || phases > OWL_PHASE_ALL) return OWL_ERR_INVALID_ARG;
+    const bool quant = k_scale != nullptr;           // a cache of 8-bit blocks
     FullPlan fp;
-    owl_status st = make_plan(desc, &fp);
+    owl_status st = make_plan(desc, &fp, quant);
     if (st != OWL_OK) return st;
     if (!q || !k_cache || !v_cache || !ctx_lens || !tree_parent || !out) return OWL_ERR_INVALID_ARG;
     if (misaligned(q, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(out, 16))
@@ -408,7 +424,7 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
     // the profiling copy of the kernel, if the timeline hook is on and has room for this grid
     const Variant *variant = fp.variant;
     const TimelineHook hook = timeline_hook();
-    if (hook.buffer && fp.pub.n_workgroups <= hook.capacity) {
+    if (hook.buffer && !quant && fp.pub.n_workgroups <= hook.capacity) {
         const Variant *tv = find_variant(variant->dtype, variant->D, variant->tpw, variant->wr, variant->wk, true);
         if (tv) variant = tv;
     }
@@ -417,8 +433,9 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
 
     // workspace: partial O | partial (m, l, s)
     char *ws = static_cast<char *>(workspace);
-    KParams p;
+    QuantParams p;
     memset(&p, 0, sizeof p);
+    p.k_scale = k_scale; p.v_scale = v_scale;
     p.q = q; p.k = k_cache; p.v = v_cache;
     p.page_table = page_table; p.ctx_lens = ctx_lens; p.parent = tree_parent;
     p.n_draft_seq = n_draft_seq;
@@ -630,6 +647,142 @@ owl_status owl_commit_kv(const owl_verify_desc *desc, void *k_cache, void *v_cac
     return OWL_OK;
 }
 
+// ---- caches of 8-bit blocks ----
+owl_status owl_verify_attn_quant(const owl_verify_desc *desc, const void *q, const void *k_cache, const void *v_cache,
+                                 const uint8_t *k_scale, const uint8_t *v_scale, const int32_t *page_table,
+                                 const int32_t *ctx_lens, const int32_t *tree_parent, const int32_t *n_draft_seq,
+                                 void *out, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream)
+{
+    if (!k_scale || !v_scale) return OWL_ERR_INVALID_ARG;
+    return verify_impl(desc, q, k_cache, v_cache, page_table, ctx_lens, tree_parent, n_draft_seq, out, workspace,
+                       workspace_bytes, dev_status, stream, OWL_PHASE_ALL, nullptr, nullptr, k_scale, v_scale);
+}
+
+owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, size_t *bytes)
+{
+    if (!bytes) return OWL_ERR_INVALID_ARG;
+    FullPlan fp;
+    const owl_status st = make_plan(desc, &fp, true);
+    if (st != OWL_OK) return st;
+    *bytes = fp.pub.workspace_bytes;
+    return OWL_OK;
+}
+
+owl_status owl_verify_attn_quant_init(const owl_verify_desc *desc)
+{
+    FullPlan fp;
+    owl_status st = make_plan(desc, &fp, true);
+    if (st != OWL_OK) return st;
+    st = ensure_lds_attr(fp.variant);
+    if (st != OWL_OK) return st;
+    return load_aux_kernels() == hipSuccess ? OWL_OK : OWL_ERR_HIP;
+}
+
+owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                               const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted,
+                               const int32_t *n_accept, int32_t *new_ctx_lens, uint32_t *dev_status, void *stream)
+{
+    const owl_status st = check_quant_desc(desc);
+    if (st != OWL_OK) return st;
+    if (!k_cache || !v_cache || !k_scale || !v_scale || !ctx_lens || !accepted || !n_accept) return OWL_ERR_INVALID_ARG;
+    if (new_ctx_lens == ctx_lens || (!page_table && desc->batch > 1)) return OWL_ERR_INVALID_ARG;
+    if (misaligned(k_cache, 16) || misaligned(v_cache, 16)) return OWL_ERR_INVALID_ARG;
+    if (desc->batch > kMaxGrid) return OWL_ERR_UNSUPPORTED;
+    if (page_table &&
+        (int64_t)desc->max_pages_per_seq * kPage < (int64_t)desc->max_ctx_len + desc->n_draft)
+        return OWL_ERR_INVALID_ARG;
+    if (launch_commit_quant(*desc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,
+                            new_ctx_lens, dev_status, static_cast<hipStream_t>(stream)) != hipSuccess)
+        return OWL_ERR_HIP;
+    return OWL_OK;
+}
+
+// ---- new rows of the cache ----
+static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc *a, const void *q, const void *k_new,
+                              const void *v_new, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
+                              void *v_cache, uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table,
+                              const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status, void *stream)
+{
+    const owl_status st = k_scale ? check_quant_desc(desc) : check_desc(desc);
+    if (st != OWL_OK) return st;
+    if (!a || !k_new || !v_new || !k_cache || !v_cache || !ctx_lens) return OWL_ERR_INVALID_ARG;
+    if ((q == nullptr) != (q_out == nullptr) || (!page_table && desc->batch > 1)) return OWL_ERR_INVALID_ARG;
+    if (a->n_tokens < 1 || a->n_tokens > (1 << 30)) return OWL_ERR_INVALID_ARG;
+    if (a->rot_dim < 0 || a->rot_dim > desc->head_dim || a->rot_dim % 16 != 0) return OWL_ERR_UNSUPPORTED;
+    if (a->rot_style != OWL_ROT_HALVES && a->rot_style != OWL_ROT_PAIRS) return OWL_ERR_UNSUPPORTED;
+    if (!isfinite(a->rot_scale) || (a->rot_dim > 0 && !inv_freq)) return OWL_ERR_INVALID_ARG;
+    const int64_t es = elem_size(desc->qkv_dtype), D = desc->head_dim;
+    const int64_t strides[3] = {q ? a->q_stride : desc->n_q_heads * D, a->k_stride, a->v_stride};
+    for (int t = 0; t < 3; ++t)
+        if (strides[t] < (t == 0 ? desc->n_q_heads : desc->n_kv_heads) * D || strides[t] * es % 16 != 0) return OWL_ERR_INVALID_ARG;
+    if (q && q == q_out && a->q_stride != desc->n_q_heads * D) return OWL_ERR_INVALID_ARG;
+    for (const void *ptr : {q, k_new, v_new, (const void *)q_out, (const void *)k_cache, (const void *)v_cache})
+        if (misaligned(ptr, 16)) return OWL_ERR_INVALID_ARG;           // a null pointer counts as aligned
+    // (with a count for each sequence n_tokens is only the longest: what lies beyond the table is found on the device)
+    if (page_table && !n_new_seq && (int64_t)desc->max_pages_per_seq * kPage < (int64_t)desc->max_ctx_len + a->n_tokens)
+        return OWL_ERR_INVALID_ARG;
+    if (desc->batch > kMaxGrid || desc->n_kv_heads > kMaxGrid) return OWL_ERR_UNSUPPORTED;
+    if (launch_append(*desc, *a, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
+                      ctx_lens, n_new_seq, dev_status, static_cast<hipStream_t>(stream)) != hipSuccess)
+        return OWL_ERR_HIP;
+    return OWL_OK;
+}
+
+owl_status owl_append_kv(const owl_verify_desc *desc, const owl_append_desc *append, const void *q, const void *k_new,
+                         const void *v_new, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
+                         void *v_cache, const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq,
+                         uint32_t *dev_status, void *stream)
+{
+    return append_impl(desc, append, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, nullptr, nullptr, page_table,
+                       ctx_lens, n_new_seq, dev_status, stream);
+}
+
+owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_desc *append, const void *q, const void *k_new,
+                               const void *v_new, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
+                               void *v_cache, uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table,
+                               const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status, void *stream)
+{
+    if (!k_scale || !v_scale) return OWL_ERR_INVALID_ARG;
+    return append_impl(desc, append, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
+                       ctx_lens, n_new_seq, dev_status, stream);
+}
+
+// ---- rows of logits ----
+static owl_status check_logprob(const owl_logprob_desc *d)
+{
+    if (!d) return OWL_ERR_INVALID_ARG;
+    if (d->rows < 1 || d->vocab < 1 || d->n_given < 0 || d->n_top < 0 || d->row_stride < d->vocab) return OWL_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || !isfinite(d->scale)) return OWL_ERR_INVALID_ARG;
+    if (d->dtype != OWL_BF16 && d->dtype != OWL_F32 && d->dtype != OWL_F16) return OWL_ERR_UNSUPPORTED;
+    if (d->n_given > 64 || d->n_top > 32 || d->vocab > (1 << 28)) return OWL_ERR_UNSUPPORTED;
+    return OWL_OK;
+}
+
+owl_status owl_token_logprobs_workspace_size(const owl_logprob_desc *desc, size_t *bytes)
+{
+    const owl_status st = check_logprob(desc);
+    if (st != OWL_OK) return st;
+    if (!bytes) return OWL_ERR_INVALID_ARG;
+    *bytes = align_up(logprob_scratch_bytes(*desc, device_cus()), 256);
+    return OWL_OK;
+}
+
+owl_status owl_token_logprobs(const owl_logprob_desc *desc, const void *logits, const int32_t *tokens, float *logprob,
+                              float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes,
+                              uint32_t *dev_status, void *stream)
+{
+    const owl_status st = check_logprob(desc);
+    if (st != OWL_OK) return st;
+    if (!logits || misaligned(logits, (size_t)elem_size(desc->dtype))) return OWL_ERR_INVALID_ARG;
+    if (desc->n_given > 0 && (!tokens || !logprob)) return OWL_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < logprob_scratch_bytes(*desc, device_cus())) return OWL_ERR_WORKSPACE;
+    if (misaligned(workspace, 256)) return OWL_ERR_INVALID_ARG;
+    if (launch_logprobs(*desc, logits, tokens, logprob, entropy, top_ids, top_logprobs, workspace, dev_status, device_cus(),
+                        static_cast<hipStream_t>(stream)) != hipSuccess)
+        return OWL_ERR_HIP;
+    return OWL_OK;
+}
+
 static owl_status check_drafter(const owl_drafter_desc *d)
 {
     if (!d) return OWL_ERR_INVALID_ARG;
@@ -770,6 +923,6 @@ const char *owl_status_str(owl_status s)
     return "unknown status";
 }
 
-const char *owl_version(void) { return "0.2"; }
+const char *owl_version(void) { return "0.3"; }
 
 }  // extern "C"

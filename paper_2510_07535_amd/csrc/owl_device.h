@@ -72,9 +72,14 @@ __device__ __forceinline__ void fetch_args()
     typedef const __attribute__((address_space(4))) int32_t *Line;
     const Line at = (Line)__builtin_amdgcn_kernarg_segment_ptr();
     constexpr int n = (bytes + 63) / 64;
-    static_assert(n <= 4, "four lines of arguments");
+    static_assert(n <= 5, "five lines of arguments");
     const int32_t a = at[0], b = at[n > 1 ? 16 : 0], c = at[n > 2 ? 32 : 0], d = at[n > 3 ? 48 : 0];
-    asm volatile("" ::"s"(a), "s"(b), "s"(c), "s"(d));
+    if constexpr (n > 4) {
+        const int32_t e = at[64];
+        asm volatile("" ::"s"(a), "s"(b), "s"(c), "s"(d), "s"(e));
+    } else {
+        asm volatile("" ::"s"(a), "s"(b), "s"(c), "s"(d));
+    }
 }
 
 // Reads through the scalar cache; for arrays no kernel of the launch writes, uniform index.

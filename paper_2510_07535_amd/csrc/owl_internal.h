@@ -51,19 +51,30 @@ struct KParams {
     long long *timeline;  // instantiations with the timeline hook only: 10 slots per workgroup (profiling aid)
 };
 
+// For caches of 8-bit blocks: the scale bytes, [page][KV head].
+struct QuantParams : KParams {
+    const uint8_t *k_scale, *v_scale;
+};
+
 // One instantiated split-KV kernel.  `timeline` marks the copies that carry the
 // per-workgroup timeline hook (profiling builds of the bf16 / D = 128 kernels);
 // the production copies have no trace of it.
 struct Variant {
     int dtype, D, tpw, wr, wk;
     bool timeline;
+    bool quant;           // reads a cache of 8-bit blocks; `launch` then takes a QuantParams
     size_t lds_bytes;
     // start / stop: optional events attached to the kernel's own dispatch (its begin and end), else null
     void (*launch)(const KParams &, dim3 grid, hipStream_t, hipEvent_t start, hipEvent_t stop);
     const void *func;     // for hipFuncSetAttribute
 };
 
-const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline = false);
+const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline = false, bool quant = false);
+struct VariantList {
+    const Variant *first;
+    int count;
+};
+VariantList quant_variants();
 int variant_index(const Variant *v);
 
 // Profiling hook state (set through the probe interface; read by the verify entry points).
@@ -84,6 +95,17 @@ hipError_t launch_accept(const int32_t *tokens, const int32_t *parent, const int
 hipError_t launch_commit(const owl_verify_desc &d, void *k_cache, void *v_cache, const int32_t *page_table,
                          const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
                          int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
+// Caches of 8-bit blocks: k_scale is null for a cache in qkv_dtype.
+hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const void *q, const void *k_new, const void *v_new,
+                         const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
+                         uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,
+                         const int32_t *n_new_seq, uint32_t *status, hipStream_t s);
+hipError_t launch_commit_quant(const owl_verify_desc &d, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                               const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted,
+                               const int32_t *n_accept, int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
+size_t logprob_scratch_bytes(const owl_logprob_desc &d, int n_cus);
+hipError_t launch_logprobs(const owl_logprob_desc &d, const void *logits, const int32_t *tokens, float *logprob, float *entropy,
+                           int32_t *top_ids, float *top_logprobs, void *scratch, uint32_t *status, int n_cus, hipStream_t s);
 hipError_t launch_drafter_proj(int dtype, const void *h, const void *w, bool tiled, float *s, int P, int d_in,
                                int d, int n_cus, hipStream_t st);
 size_t drafter_tiled_bytes(int d_in, int d);

@@ -1,0 +1,243 @@
+"""The verify attention over caches of 8-bit blocks and the commit in them, against the oracles.  Needs an MI355X (-m gpu)."""
+import numpy as np
+import pytest
+import torch
+
+from block_helpers import DEV, NAN_BYTE, QuantStep, assert_attention, block_case, i32, oracle_out, rng
+from oracle import cache_blocks as C
+from paper_2510_07535_amd import binding as B
+from paper_2510_07535_amd import workloads as W
+
+pytestmark = pytest.mark.gpu
+
+
+def _trees(kind, n, count, r):
+    return [W.chain_tree(n) if kind == "chain" or (kind == "mix" and i % 2) else W.random_tree(n, 6, r) for i in range(count)]
+
+
+# --------------------------------------------------------------------------- attention
+# rows per KV head from one tile to several row groups, pieces shorter and longer than a page, odd lengths
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,group,hkv,ctx", [
+    (1, 4, 2, [0]), (1, 1, 1, [1]), (1, 4, 2, [15]), (3, 4, 2, [16]), (6, 4, 2, [17]), (4, 8, 1, [63]), (60, 1, 2, [64]), (16, 4, 2, [1000]),
+    (26, 4, 2, [2047]), (40, 4, 1, [700]), (40, 8, 2, [1500]), (60, 8, 1, [900]), (64, 8, 1, [333]), (5, 3, 3, [5003]), (2, 4, 8, [4500]),
+])
+def test_attention_matches_the_oracle(dtype, D, n, group, hkv, ctx):
+    r = rng(n * 1000 + D + dtype)
+    bc = block_case("quant", 7 + n, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=D, ctx_lens=ctx, trees=_trees("tree", n, 1, r),
+                    head_major=n % 2 == 0, spare_pages=3)
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc), f"{n} {group} {hkv} {ctx}")
+    assert step.flags() == 0
+
+
+@pytest.mark.parametrize("dtype,D,n,group,hkv,ctx,split", [
+    (W.DT_BF16, 128, 26, 4, 2, [0, 1, 700, 33, 1029], 0), (W.DT_F16, 128, 7, 4, 2, [300, 0, 0, 2000], 0),
+    (W.DT_BF16, 64, 40, 8, 1, [500, 16, 48, 15, 17, 900], 0), (W.DT_F16, 64, 12, 4, 4, [640] * 9, 0),
+    (W.DT_BF16, 128, 20, 8, 2, [513, 64, 65], 128), (W.DT_F16, 128, 60, 4, 1, [1300, 77], 192),
+])
+def test_batches_with_drafts_of_different_sizes(dtype, D, n, group, hkv, ctx, split):
+    r = rng(len(ctx) * 100 + n)
+    bc = block_case("quant-batch", 31 + n, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=D, ctx_lens=ctx, trees=_trees("mix", n, len(ctx), r))
+    for counts in (None, r.integers(0, n + 1, len(ctx))):
+        step = QuantStep(bc, counts=counts, split_tokens=split, flags=B.OWL_FLAG_FP32_PARTIALS if split else 0)
+        step.run()
+        assert_attention(step.result(), bc, oracle_out(bc, counts), str(counts))
+        assert step.flags() == 0
+
+
+@pytest.mark.parametrize("n,group,hkv,ctx", [(26, 4, 2, 20000), (60, 4, 2, 9000), (40, 8, 1, 30000), (6, 4, 1, 40000)])
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+def test_long_contexts(n, group, hkv, ctx, dtype):
+    """Many stages a piece, pairs of wavefronts, row groups: against the 16-bit path's oracle on sampled rows."""
+    import oracle
+    from util import sample_rows
+    r = rng(ctx)
+    bc = block_case("quant-long", ctx, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=128, ctx_lens=[ctx], trees=_trees("tree", n, 1, r), outlier_frac=0.02)
+    step = QuantStep(bc)
+    step.run()
+    got, rows = step.result(), sample_rows(bc.case, 64)
+    want = oracle.verify_attn_case(bc.case, rows=rows)
+    assert_attention(got[rows[:, 0], rows[:, 1], rows[:, 2]], bc, want)
+    assert np.isfinite(got).all() and step.flags() == 0
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("group,n", [(4, 6), (4, 26), (8, 40)])
+def test_pages_of_very_different_scales(dtype, group, n):
+    """Neighbouring pages differ by up to 2^10 (fp16: 2^6) in their scales, of K and of V each."""
+    r = rng(5 * n)
+    top = 5 if dtype == W.DT_BF16 else 3
+    bc = block_case("quant-scales", 3, page_gain=lambda g, k: 2.0 ** g.integers(-top, top + 1, k), dtype=dtype, Hq=2 * group, Hkv=2, D=128,
+                    ctx_lens=[1111], trees=_trees("tree", n, 1, r), scale=0.02)
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
+@pytest.mark.parametrize("group,n,ctx", [(4, 5, 3000), (4, 26, 2500), (8, 40, 1800), (4, 60, 1200)])
+def test_fp16_scores_that_outgrow_the_first_ones(group, n, ctx):
+    """Late keys far longer than the early ones: the frozen references of the fp16 loops overflow and pieces are redone."""
+    r = rng(ctx)
+    bc = block_case("quant-overflow", 17, page_gain=None, dtype=W.DT_F16, Hq=2 * group, Hkv=2, D=128, ctx_lens=[ctx],
+                    trees=_trees("tree", n, 1, r), outlier_frac=0.05, outlier_gain=16.0)
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
+def test_answers_in_16_bits_and_zeros_of_absent_nodes():
+    r = rng(1)
+    for dtype, kind in ((W.DT_BF16, B.OWL_BF16), (W.DT_F16, B.OWL_F16)):
+        bc = block_case("quant-out", 5, dtype=dtype, Hq=8, Hkv=2, D=128, ctx_lens=[300, 20], trees=_trees("tree", 9, 2, r))
+        full, half = QuantStep(bc, counts=[9, 4]), QuantStep(bc, out_dtype=kind, counts=[9, 4])
+        full.run()
+        half.run()
+        want = full.out.to(half.out.dtype)
+        torch.cuda.synchronize()
+        assert torch.equal(half.out, want) and not half.out[1, 4:].any()
+
+
+def test_identity_paging():
+    bc = block_case("quant-flat", 8, dtype=W.DT_BF16, Hq=4, Hkv=1, D=128, ctx_lens=[777], trees=[W.chain_tree(4)], paged=False, head_major=False)
+    assert bc.case.page_table is None
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
+def test_bad_pages_lengths_and_counts_are_flagged_and_stay_in_bounds():
+    r = rng(2)
+    bc = block_case("quant-bad", 9, dtype=W.DT_BF16, Hq=8, Hkv=2, D=128, ctx_lens=[400, 200], trees=_trees("tree", 5, 2, r))
+    ref = QuantStep(bc)
+    ref.run()
+    want = ref.result()
+    step = QuantStep(bc)
+    step.table[0, 3] = bc.case.n_pool_pages
+    step.run()
+    got = step.result()
+    assert step.flags() == B.OWL_DEV_BAD_PAGE and np.array_equal(got[1], want[1])
+    step = QuantStep(bc, counts=[9, -1])
+    step.run()
+    assert not step.result()[1].any() and step.flags() == B.OWL_DEV_BAD_NDRAFT
+    step = QuantStep(bc)
+    step.lens[1] = 100000
+    step.run()
+    assert np.array_equal(step.result()[0], want[0]) and step.flags() & B.OWL_DEV_BAD_CTX_LEN
+
+
+def test_graph_replays_match_eager():
+    r = rng(3)
+    bc = block_case("quant-graph", 61, dtype=W.DT_BF16, Hq=16, Hkv=4, D=128, ctx_lens=[1500, 40, 700], trees=_trees("tree", 12, 3, r))
+    step = QuantStep(bc)
+    B.owl_verify_attn_quant_init(step.desc)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            step.run()
+    torch.cuda.synchronize()
+    for rep in range(4):
+        step.lens.copy_(torch.tensor([1500 - 100 * rep, 40, 700 - 300 * (rep % 2)], dtype=torch.int32))
+        step.ks.copy_(torch.from_numpy(bc.k.scale + np.where(bc.k.scale < 200, rep % 3, 0).astype(np.uint8)))
+        step.out.fill_(float("nan"))
+        graph.replay()
+        got = step.result()
+        step.out.fill_(float("nan"))
+        step.run()
+        assert np.array_equal(got, step.result()), rep
+    assert step.flags() == 0
+
+
+# --------------------------------------------------------------------------- commit
+def _commit(bc, acc, na, table=None, new=True):
+    c = bc.case
+    step = QuantStep(bc)
+    if table is not None:
+        step.table = i32(table)
+    new_lens = torch.full((c.B,), -7, dtype=torch.int32, device=DEV) if new else None
+    B.owl_commit_kv_quant(step.desc, step.k, step.v, step.ks, step.vs, step.table, step.lens, i32(acc), i32(na), new_lens, step.status)
+    return step, new_lens
+
+
+def _same(step, k, v):
+    torch.cuda.synchronize()
+    for got, scale, want in ((step.k, step.ks, k), (step.v, step.vs, v)):
+        assert np.array_equal(scale.cpu().numpy(), want.scale)
+        assert C.same_bytes(got.cpu().numpy(), want.flat)
+
+
+def _paths(B_, N, r, most):
+    acc, na = np.full((B_, N), -1, np.int32), np.zeros(B_, np.int32)
+    for b in range(B_):
+        na[b] = r.integers(0, most + 1)
+        acc[b, :na[b]] = np.sort(r.choice(N, na[b], replace=False))
+    return acc, na
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N,most,head_major", [(1, 1, True), (6, 6, True), (40, 8, False), (64, 64, True), (64, 20, False)])
+def test_commit_matches_the_oracle(dtype, D, N, most, head_major):
+    r = rng(N * 10 + D + dtype)
+    ctx = [0, 1, 15, 16, 31, 100, 333]
+    bc = block_case("commit", N, page_gain=lambda g, k: 2.0 ** g.integers(-9, 7, k), dtype=dtype, Hq=3, Hkv=3, D=D, ctx_lens=ctx,
+                    trees=[W.chain_tree(N)] * len(ctx), head_major=head_major, spare_pages=2)
+    acc, na = _paths(len(ctx), N, r, most)
+    if N == 64 and most == 64:
+        acc[0], na[0] = np.arange(64), 64                # all in place
+        acc[2, :63], na[2] = np.arange(1, 64), 63        # all move by one
+        acc[2, 63] = -1
+        na[4], acc[4] = 0, -1
+    k, v = bc.k.copy(), bc.v.copy()
+    for blocks in (k, v):
+        blocks.commit(bc.case.page_table, bc.case.ctx_lens, acc, na)
+    step, new_lens = _commit(bc, acc, na)
+    _same(step, k, v)
+    assert step.flags() == 0 and new_lens.cpu().numpy().tolist() == (bc.case.ctx_lens + na).tolist()
+
+
+def test_commit_without_lengths_and_with_identity_paging():
+    bc = block_case("commit-flat", 4, dtype=W.DT_BF16, Hq=2, Hkv=2, D=128, ctx_lens=[21], trees=[W.chain_tree(20)], paged=False)
+    acc, na = np.full((1, 20), -1, np.int32), np.array([3], np.int32)
+    acc[0, :3] = [2, 9, 19]
+    k, v = bc.k.copy(), bc.v.copy()
+    for blocks in (k, v):
+        blocks.commit(None, [21], acc, na)
+    step, _ = _commit(bc, acc, na, new=False)
+    _same(step, k, v)
+
+
+def test_commit_flags_bad_lists_pages_and_lengths_and_moves_nothing_there():
+    r = rng(8)
+    bc = block_case("commit-bad", 6, dtype=W.DT_BF16, Hq=2, Hkv=2, D=64, ctx_lens=[30, 100, 50, 60], trees=[W.chain_tree(12)] * 4)
+    acc, na = np.full((4, 12), -1, np.int32), np.array([2, 3, 2, 2], np.int32)
+    acc[0, :2], acc[1, :3], acc[2, :2], acc[3, :2] = [3, 3], [0, 1, 12], [4, 7], [5, 11]
+    table = bc.case.page_table.copy()
+    table[3, (60 + 11) // 16] = -1
+    k, v = bc.k.copy(), bc.v.copy()
+    for blocks in (k, v):
+        blocks.commit(bc.case.page_table, bc.case.ctx_lens, acc, [0, 0, 2, 0])
+    step, new_lens = _commit(bc, acc, na, table=table)
+    _same(step, k, v)
+    assert step.flags() == B.OWL_DEV_BAD_ACCEPT | B.OWL_DEV_BAD_PAGE
+    assert new_lens.cpu().numpy().tolist() == [30, 100, 52, 60]
+    step, new_lens = _commit(bc, acc, np.array([0, 99, 0, -3], np.int32))
+    _same(step, bc.k, bc.v)
+    assert step.flags() == B.OWL_DEV_BAD_ACCEPT
+
+
+def test_a_second_commit_of_rows_in_place_changes_nothing():
+    r = rng(12)
+    bc = block_case("commit-twice", 14, dtype=W.DT_F16, Hq=2, Hkv=2, D=128, ctx_lens=[45], trees=[W.chain_tree(10)])
+    acc, na = np.full((1, 10), -1, np.int32), np.array([4], np.int32)
+    acc[0, :4] = [1, 4, 5, 9]
+    step, _ = _commit(bc, acc, na)
+    torch.cuda.synchronize()
+    before = [x.clone() for x in (step.k, step.v, step.ks, step.vs)]
+    B.owl_commit_kv_quant(step.desc, step.k, step.v, step.ks, step.vs, step.table, step.lens, i32([[0, 1, 2, 3] + [-1] * 6]), i32(na), None, step.status)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, (step.k, step.v, step.ks, step.vs)))
