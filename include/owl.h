@@ -376,8 +376,9 @@ owl_status owl_append_kv(const owl_verify_desc *desc, const owl_append_desc *app
  * (uint8, contiguous, n_pool_pages * Hkv of them).  A cached number is
  *     e4m3(byte) * 2^(s - 127) ,   1 <= s <= 254,
  * in qkv_dtype, which is OWL_BF16 or OWL_F16 here.  In a descriptor for such a
- * cache the kv strides count bytes, and are multiples of 16.  Half the memory and
- * traffic of a 16-bit cache.  The calls that write a block choose its scale from
+ * cache the kv strides count bytes, and are multiples of 16; kv_stride_token is at
+ * most 2^26.  Half the memory and traffic of a 16-bit cache.  The calls that write
+ * a block choose its scale from
  * all rows that count in it, as
  *     the least e >= e0 with  max |number| <= 448 * 2^e ,    s = e + 127 ,
  * e0 = -117 (OWL_BF16) or -15 (OWL_F16), and round to nearest even.  Powers of

@@ -77,6 +77,7 @@ owl_status check_quant_desc(const owl_verify_desc *d)
     if (d->qkv_dtype == OWL_F32) return OWL_ERR_UNSUPPORTED;
     for (int64_t s : {d->kv_stride_page, d->kv_stride_head, d->kv_stride_token})
         if (s % 16 != 0) return OWL_ERR_INVALID_ARG;
+    if (d->kv_stride_token > (1 << 26)) return OWL_ERR_UNSUPPORTED;      // offsets within a page are 32 bits wide
     return OWL_OK;
 }
 
@@ -100,7 +101,17 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // outgrowing the K/V they summarise: then the rows are cut into more, smaller
     // groups instead, each re-reading the split from its XCD's L2.
     int tpw, wr, wk, rgs, group_tiles;
-    if (d->qkv_dtype == OWL_F32) {
+    // Over 8-bit blocks few tiles go to wavefronts with keys of their own, two tiles a row group (owl_splitkv_few.hip), many to
+    // the shared ring.  us, ring -> own keys, 8 KV heads, head_dim 128: 64K context, 1 tile 40.5 -> 27.3, 3 44.0 -> 39.8, 4 44.8 ->
+    // 40.8, 5 59.1 -> 51.5, 6 60.6 -> 52.0, 7 61.7 -> 59.8, 8 62.8 -> 60.3, and 15 in groups of two 84.5 -> 99.7; 8 tiles of 1 KV head
+    // 22.0 -> 17.6; 16 sequences of 8K-64K, 1 tile 309 -> 213, 3 331 -> 296, 4 336 -> 303, 5 469 -> 421, but 7 399 -> 499 (four groups
+    // read each key from L2, and in a batch nothing else is short of time).
+    const bool few = quant && RT <= (d->batch == 1 ? 8 : 6);
+    if (few) {
+        rgs = (RT + 1) / 2;
+        group_tiles = (RT + rgs - 1) / rgs;
+        tpw = group_tiles; wr = rgs > 1 ? 2 : 1; wk = 8;
+    } else if (d->qkv_dtype == OWL_F32) {
         tpw = 1; wr = 8; wk = 1; rgs = (RT + 7) / 8;
         group_tiles = (RT + rgs - 1) / rgs;
     } else {
@@ -239,7 +250,9 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     }
     // Workspace: the partials that are written, and never less than equal splits of half the planned size
     // would need for a batch (the planned size for one sequence).
-    fp->half_partials = d->qkv_dtype != OWL_F32 && !(d->flags & OWL_FLAG_FP32_PARTIALS);
+    // (8-bit blocks: own keys leave fp32 partials; and with fp16 queries, whose answer keeps 11 bits, fp16 partials would cost as much as
+    // its own rounding, 3.4e-4 instead of 2.1e-4 in all, for 2.5 % of the time)
+    fp->half_partials = d->qkv_dtype != OWL_F32 && !few && !(quant && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
     const size_t o_bytes = (size_t)d->head_dim * kRowTile * (fp->half_partials ? 2 : 4), ml_bytes = kPartMl * sizeof(float);
     auto bytes_of = [&](size_t slots, size_t unit) -> size_t { return align_up((size_t)d->n_kv_heads * slots * RT * unit, 256); };
     auto partials = [&](size_t slots) -> size_t { return bytes_of(slots, o_bytes) + bytes_of(slots, ml_bytes); };
@@ -296,11 +309,11 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
 owl_status ensure_lds_attr(const Variant *v)
 {
     static std::mutex mu;
-    static bool done[16][64] = {};
+    static bool done[16][80] = {};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return OWL_ERR_HIP;
     const int vi = variant_index(v);
-    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 64) return OWL_ERR_HIP;
+    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 80) return OWL_ERR_HIP;
     std::lock_guard<std::mutex> lock(mu);
     if (!done[dev][vi]) {
         if (hipFuncSetAttribute(v->func, hipFuncAttributeMaxDynamicSharedMemorySize,

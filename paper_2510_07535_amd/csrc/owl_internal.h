@@ -74,7 +74,8 @@ struct VariantList {
     const Variant *first;
     int count;
 };
-VariantList quant_variants();
+VariantList quant_variants();      // owl_splitkv_quant.hip
+VariantList few_tile_variants();   // owl_splitkv_few.hip: caches of 8-bit blocks too, wr = 1, wk = 8
 int variant_index(const Variant *v);
 
 // Profiling hook state (set through the probe interface; read by the verify entry points).

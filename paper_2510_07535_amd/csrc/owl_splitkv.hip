@@ -17,10 +17,9 @@ constexpr int kCount = sizeof kVariants / sizeof kVariants[0];
 
 const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline, bool quant)
 {
-    const VariantList quantised = quant_variants();
-    const Variant *list = quant ? quantised.first : kVariants;
-    for (int i = 0; i < (quant ? quantised.count : kCount); ++i) {
-        const Variant &v = list[i];
+    const VariantList list = !quant ? VariantList{kVariants, kCount} : wk == kWaves ? few_tile_variants() : quant_variants();
+    for (int i = 0; i < list.count; ++i) {
+        const Variant &v = list.first[i];
         if (v.dtype == dtype && v.D == D && v.tpw == tpw && v.wr == wr && v.wk == wk && v.timeline == timeline) return &v;
     }
     return nullptr;
@@ -29,7 +28,9 @@ const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool time
 int variant_index(const Variant *v)
 {
     if (!v) return -1;
-    return static_cast<int>(v->quant ? kCount + (v - quant_variants().first) : v - kVariants);
+    if (!v->quant) return static_cast<int>(v - kVariants);
+    const VariantList quant = quant_variants();
+    return static_cast<int>(v->wk == kWaves ? kCount + quant.count + (v - few_tile_variants().first) : kCount + (v - quant.first));
 }
 
 }  // namespace owl

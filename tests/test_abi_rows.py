@@ -66,6 +66,13 @@ def test_append_refuses_descriptors(quant):
     assert _append(_desc(n_q_heads=7), _append_desc(), quant) == B.OWL_ERR_INVALID_ARG
 
 
+def test_8_bit_blocks_refuse_token_strides_beyond_32_bit_page_offsets():
+    d = _desc(kv_stride_token=(1 << 26) + 16)
+    assert _append(d, _append_desc(), True) == B.OWL_ERR_UNSUPPORTED
+    with pytest.raises(B.OwlError):
+        B.owl_verify_attn_quant_workspace_size(d)
+
+
 def test_8_bit_blocks_refuse_32_bit_numbers_odd_strides_and_missing_scales():
     for d, code in ((_desc(qkv_dtype=B.OWL_F32), B.OWL_ERR_UNSUPPORTED), (_desc(kv_stride_token=136), B.OWL_ERR_INVALID_ARG),
                     (_desc(kv_stride_head=16 * 128 + 8), B.OWL_ERR_INVALID_ARG)):

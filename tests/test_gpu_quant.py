@@ -88,6 +88,18 @@ def test_fp16_scores_that_outgrow_the_first_ones(group, n, ctx):
     assert_attention(step.result(), bc, oracle_out(bc))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("ctx", [[2111], [900, 31, 1500]])
+@pytest.mark.parametrize("n", [4, 8, 11, 16, 20, 24, 28, 32, 36])
+def test_every_number_of_row_tiles(n, ctx, D):
+    r = rng(n * 3 + D)
+    bc = block_case("quant-tiles", n + D, dtype=W.DT_F16 if n % 8 else W.DT_BF16, Hq=8, Hkv=2, D=D, ctx_lens=ctx, trees=_trees("tree", n, len(ctx), r))
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+    assert step.flags() == 0
+
+
 def test_answers_in_16_bits_and_zeros_of_absent_nodes():
     r = rng(1)
     for dtype, kind in ((W.DT_BF16, B.OWL_BF16), (W.DT_F16, B.OWL_F16)):
