@@ -850,6 +850,11 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     };
 
     // ---- reference m of every row tile from one unmasked step (before the fast loop) ----
+    // 8-bit blocks, bf16: the reference lies 2^40 above the first step's maximum.  Weights of 2^-40 are as exact as others (what is
+    // lost is 2^-86 of a row's first maximum), and a score may lie 140 above it, not 100.  Keys of eight times the usual length, one
+    // in 20 of 128K, reach 135 now and then, and the redo of a piece takes the call from 201 to 303-504 us.  (A 16-bit cache
+    // keeps its results, bit for bit.)
+    constexpr float kLift = kQuant && !kGuard ? 40.0f : 0.0f;
     auto init_reference = [&](int buf, int ks, [[maybe_unused]] float head_room, f32x4 (&keep)[TPW][2]) {
         if constexpr (!kF32) {
             // (Formed here: as an address that the compiler kept from before the stages were requested, it came back from
@@ -873,7 +878,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                 const float tm = highest(s0, s1);
                 // fp16 holds 2^(x - m) only up to 2^16: its reference sits a little above the
                 // first step's maximum, which trades low-end resolution for head room
-                m[t] = quad_column_max(tm) * c_log2 + (kGuard ? head_room : 0.0f);
+                m[t] = quad_column_max(tm) * c_log2 + (kGuard ? head_room : kLift);
                 if constexpr (kGuard) wide |= is_wide(s0, s1, tm);
             }
             if constexpr (kGuard) alarm(wide, 0);

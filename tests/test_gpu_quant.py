@@ -88,6 +88,18 @@ def test_fp16_scores_that_outgrow_the_first_ones(group, n, ctx):
     assert_attention(step.result(), bc, oracle_out(bc))
 
 
+@pytest.mark.parametrize("gain", [8.0, 32.0, 64.0])
+@pytest.mark.parametrize("group,n,ctx", [(4, 5, 3000), (4, 26, 2500), (8, 40, 1800), (4, 60, 1200)])
+def test_bf16_scores_that_outgrow_the_first_ones(group, n, ctx, gain):
+    """The same in bf16, with its exponents: scores that lie some 40, 160 and 320 (as powers of two) above the first ones."""
+    r = rng(ctx + int(gain))
+    bc = block_case("quant-overflow", 17, page_gain=None, dtype=W.DT_BF16, Hq=2 * group, Hkv=2, D=128, ctx_lens=[ctx],
+                    trees=_trees("tree", n, 1, r), outlier_frac=0.05, outlier_gain=gain)
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("ctx", [[2111], [900, 31, 1500]])
 @pytest.mark.parametrize("n", [4, 8, 11, 16, 20, 24, 28, 32, 36])
