@@ -451,7 +451,7 @@ owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void 
  * Sums are formed in float32, in an order that depends on the shape only.
  */
 typedef struct owl_logprob_desc {
-    int32_t rows, vocab;      /* >= 1                                       */
+    int32_t rows, vocab;      /* >= 1; vocab <= 2^20                        */
     int32_t n_given, n_top;
     int32_t dtype;            /* owl_dtype of the logits                    */
     float scale;              /* one over the temperature; finite, positive */

@@ -767,7 +767,7 @@ static owl_status check_logprob(const owl_logprob_desc *d)
     if (d->rows < 1 || d->vocab < 1 || d->n_given < 0 || d->n_top < 0 || d->row_stride < d->vocab) return OWL_ERR_INVALID_ARG;
     if (!(d->scale > 0.0f) || !isfinite(d->scale)) return OWL_ERR_INVALID_ARG;
     if (d->dtype != OWL_BF16 && d->dtype != OWL_F32 && d->dtype != OWL_F16) return OWL_ERR_UNSUPPORTED;
-    if (d->n_given > 64 || d->n_top > 32 || d->vocab > (1 << 28)) return OWL_ERR_UNSUPPORTED;
+    if (d->n_given > 64 || d->n_top > 32 || d->vocab > (1 << 20)) return OWL_ERR_UNSUPPORTED;
     return OWL_OK;
 }
 

@@ -6,6 +6,8 @@
 // and leaves (m, l, t) and the slice's greatest logits in the scratch; the second, a workgroup a row, joins them with
 //     M = max m_s,  w_s = e^(m_s - M),  L = sum w_s l_s,  T = sum w_s (t_s + (m_s - M) l_s)
 // and picks the greatest of the slices' greatest.
+#include <float.h>
+
 #include <type_traits>
 
 #include "owl_device.h"
@@ -16,23 +18,33 @@ typedef _Float16 l_f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kLogThreads = 256, kLogWaves = kLogThreads / 64;
 constexpr int kLogHeld = 32;                                 // logits a thread holds
+constexpr int kLogFound = 64;                                // candidates of a wavefront for the slice's greatest
+constexpr int kLogTop = 32;                                  // the most alternatives asked for
 constexpr int kSlice = kLogThreads * kLogHeld;
 constexpr float kLog2e = 1.4426950408889634f;
 // Below this e^x is 0, and x stands for -infinity: what is excluded adds 0, not 0 times infinity.
 constexpr float kFloor = -1.0e4f;
 
+// Logits as integers of the same order, 0 standing for what is no number with a sign; -0 and +0 are equal.
+__device__ __forceinline__ uint32_t logit_order(float x)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, x + 0.0f);
+    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+__device__ __forceinline__ float order_logit(uint32_t order)
+{
+    return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7FFFFFFFu : ~order);
+}
+
 // A logit and its token in one number that orders them: greater logits first, smaller tokens first among equals.  0: none.
 __device__ __forceinline__ uint64_t rank_key(float x, uint32_t token)
 {
     if (!(x > -INFINITY)) return 0;
-    const uint32_t bits = __builtin_bit_cast(uint32_t, x + 0.0f);        // (-0 and +0 are equal)
-    const uint32_t order = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
-    return ((uint64_t)order << 32) | (0xFFFFFFFFu - token);
+    return ((uint64_t)logit_order(x) << 32) | (0xFFFFFFFFu - token);
 }
 __device__ __forceinline__ float key_logit(uint64_t key)
 {
-    const uint32_t order = (uint32_t)(key >> 32);
-    return __builtin_bit_cast(float, order & 0x80000000u ? order & 0x7FFFFFFFu : ~order);
+    return order_logit((uint32_t)(key >> 32));
 }
 __device__ __forceinline__ int key_token(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 
@@ -60,6 +72,28 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t v)
     return v;
 }
 
+// A number that at least `want` (<= 64) of the lanes' numbers reach, the wavefront's greatest being that of `most`: the
+// interval is halved until hardly more than `want` of them do.
+__device__ __forceinline__ uint32_t reached_by(uint32_t order, float most, int want)
+{
+    uint32_t lo = 0, hi = __builtin_amdgcn_readfirstlane(logit_order(most)) + 1;     // (all reach lo, none hi)
+    // the first step goes down from the greatest by a quarter, an octave and a half for a number of the usual size
+    uint32_t step = 3u << 22;
+    while (hi - lo > 1) {
+        const uint32_t mid = step && hi - lo > step ? hi - step : lo + (hi - lo) / 2;
+        const int count = __builtin_popcountll(__builtin_amdgcn_ballot_w64(order >= mid));
+        if (count >= want) {
+            lo = mid;
+            step = 0;
+            if (count <= want + want / 8) break;
+        } else {
+            hi = mid;
+            step *= 2;
+        }
+    }
+    return lo;
+}
+
 template <typename T>
 __device__ __forceinline__ float to_float(T x) { return (float)x; }
 
@@ -75,7 +109,9 @@ __global__ void __launch_bounds__(kLogThreads) logprob_slice_kernel(const T *log
 {
     constexpr int E = 16 / sizeof(T), kLoads = kLogHeld / E;
     __shared__ float s_m[kLogWaves], s_l[kLogWaves], s_t[kLogWaves];
-    __shared__ uint64_t s_key[kLogWaves];
+    __shared__ uint32_t s_all[kLogWaves], s_some[kLogWaves];
+    __shared__ int s_own[kLogWaves];
+    __shared__ uint64_t s_key[kLogWaves], s_found[kLogWaves][kLogFound];
     const int r = blockIdx.x, slice = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const T *row = logits + (int64_t)r * row_stride;
     // 16-byte pieces at aligned addresses: piece 0 begins `skew` logits before the row
@@ -96,27 +132,34 @@ __global__ void __launch_bounds__(kLogThreads) logprob_slice_kernel(const T *log
             for (int e = 0; e < E; ++e) x[k * E + e] = first + e >= 0 && first + e < vocab ? to_float(row[first + e]) : -INFINITY;
         }
     }
-    float top = -INFINITY;
-    bool bad = false;
+    float top = x[0];
 #pragma unroll
-    for (int k = 0; k < kLogHeld; ++k) {
-        top = fmaxf(top, x[k]);
-        bad |= !(x[k] < INFINITY);
-    }
+    for (int k = 1; k < kLogHeld; ++k) top = fmaxf(top, x[k]);
     const float wm = wave_fmax(top);
-    const bool wave_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-    if (lane == 0) s_m[wave] = wave_bad ? INFINITY : wm;
+    if (n_top > 0) {
+        // Two bounds that n_top logits of the slice reach: those of n_top threads of one wavefront, and of a quarter of
+        // them in each.  The greater one is the better: with the logits in no order the second, and where one wavefront
+        // has all the great ones the first.
+        const uint32_t order = logit_order(top);
+        const uint32_t all = reached_by(order, wm, n_top), some = reached_by(order, wm, (n_top + kLogWaves - 1) / kLogWaves);
+        if (lane == 0) {
+            s_all[wave] = all;
+            s_some[wave] = some;
+        }
+    }
+    if (lane == 0) s_m[wave] = wm;
     __syncthreads();
     float m = s_m[0];
 #pragma unroll
     for (int w = 1; w < kLogWaves; ++w) m = fmaxf(m, s_m[w]);
+    const float to_log2 = fminf(scale * kLog2e, FLT_MAX), base = m > -INFINITY ? m : 0.f;
     m *= scale;
-    const float base = m > -INFINITY ? m : 0.f;
     float l = 0.f, t = 0.f;
 #pragma unroll
     for (int k = 0; k < kLogHeld; ++k) {
-        const float y = fmaxf(__builtin_fmaf(x[k], scale, -base), kFloor);
-        const float e = __builtin_amdgcn_exp2f(y * kLog2e);
+        // (maximum keeps what is no number, and the sums tell)
+        const float y = __builtin_elementwise_maximum((x[k] - base) * to_log2, kFloor);
+        const float e = __builtin_amdgcn_exp2f(y);
         l += e;
         t = __builtin_fmaf(y, e, t);
     }
@@ -126,6 +169,26 @@ __global__ void __launch_bounds__(kLogThreads) logprob_slice_kernel(const T *log
         s_l[wave] = l;
         s_t[wave] = t;
     }
+    int own = 0;
+    if (n_top > 0) {
+        uint32_t all = s_all[0], some = s_some[0];
+#pragma unroll
+        for (int w = 1; w < kLogWaves; ++w) {
+            all = max(all, s_all[w]);
+            some = min(some, s_some[w]);
+        }
+        const float least = fmaxf(order_logit(max(all, some)), -FLT_MAX);
+#pragma unroll
+        for (int k = 0; k < kLogHeld; ++k) {
+            const uint64_t hit = __builtin_amdgcn_ballot_w64(x[k] >= least);
+            if (hit) {                               // (uniform)
+                const int place = own + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+                if (x[k] >= least && place < kLogFound) s_found[wave][place] = rank_key(x[k], (uint32_t)token_of(k));
+                own += __builtin_popcountll(hit);
+            }
+        }
+        if (lane == 0) s_own[wave] = own;
+    }
     __syncthreads();
     if (tid == 0) {
         float ls = 0.f, ts = 0.f;
@@ -134,11 +197,32 @@ __global__ void __launch_bounds__(kLogThreads) logprob_slice_kernel(const T *log
             ls += s_l[w];
             ts += s_t[w];
         }
-        stats[(int64_t)r * slices + slice] = SliceStats{m, ls, ts, m == INFINITY ? 1u : 0u};
+        const bool bad = !(ls < INFINITY) || m == INFINITY;
+        stats[(int64_t)r * slices + slice] = SliceStats{bad ? INFINITY : m, ls, ts * (1.0f / kLog2e), bad ? 1u : 0u};
     }
-    // the greatest, one after the other
-    uint64_t last = ~(uint64_t)0;
+    if (n_top == 0) return;
     uint64_t *out = keys + ((int64_t)r * slices + slice) * n_top;
+    int found = 0;
+    bool fits = true;
+#pragma unroll
+    for (int w = 0; w < kLogWaves; ++w) {
+        found += s_own[w];
+        fits &= s_own[w] <= kLogFound;
+    }
+    if (fits) {
+        for (int i = lane; i < s_own[wave]; i += 64) {
+            const uint64_t key = s_found[wave][i];
+            int place = 0;                           // the number of greater ones
+#pragma unroll
+            for (int w = 0; w < kLogWaves; ++w)
+                for (int o = 0; o < s_own[w]; ++o) place += s_found[w][o] > key ? 1 : 0;
+            if (place < n_top) out[place] = key;
+        }
+        for (int j = found + tid; j < n_top; j += kLogThreads) out[j] = 0;
+        return;
+    }
+    // many equal logits: one after the other
+    uint64_t last = ~(uint64_t)0;
     for (int j = 0; j < n_top; ++j) {
         uint64_t best = 0;
 #pragma unroll
@@ -165,6 +249,9 @@ __global__ void __launch_bounds__(kLogThreads) logprob_join_kernel(const T *logi
                                                                   uint32_t *status)
 {
     __shared__ float s_l[kLogWaves], s_t[kLogWaves], s_m[kLogWaves];
+    __shared__ unsigned long long s_least;
+    __shared__ int s_count;
+    __shared__ uint64_t s_keys[kLogTop * kLogTop];   // (keys that reach the bound are those of n_top lists at most)
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const SliceStats *mine = stats + (int64_t)r * slices;
     float m = -INFINITY;
@@ -212,23 +299,46 @@ __global__ void __launch_bounds__(kLogThreads) logprob_join_kernel(const T *logi
         if (!known && token != -1) flag_status(status, OWL_DEV_BAD_TOKEN);
         logprob[(int64_t)r * n_given + j] = known ? logp(to_float(logits[(int64_t)r * row_stride + token])) : (token == -1 ? 0.f : nan);
     }
-    // a key's place is the number of greater ones
+    if (n_top == 0) return;
+    // The slices' lists are ordered.  What i + 1 of their first reach in ceil(n_top / (i + 1)) lists, n_top keys reach: the
+    // greatest such bound, of the first columns (a thread a key), leaves little more than the answer.
     const uint64_t *all = keys + (int64_t)r * slices * n_top;
-    const int count = slices * n_top;
-    int found = 0;
+    const int count = slices * n_top, columns = min(n_top, kLogThreads / slices);
+    if (tid == 0) {
+        s_least = 1;
+        s_count = 0;
+    }
+    const int i = tid / slices;
+    const bool holds = i < columns;
+    const uint64_t mine_key = holds ? all[(tid - i * slices) * n_top + i] : 0;
+    s_keys[tid] = mine_key;
+    __syncthreads();
+    if (holds && mine_key) {
+        const int lists = (n_top + i) / (i + 1);
+        int place = 0;
+        for (int o = 0; o < slices; ++o) place += s_keys[i * slices + o] > mine_key ? 1 : 0;
+        if (place == lists - 1) atomicMax(&s_least, (unsigned long long)mine_key);
+    }
+    __syncthreads();
+    const uint64_t least = s_least;
+    for (int k = tid; k < count; k += kLogThreads) {
+        const uint64_t key = all[k];
+        if (key >= least) s_keys[atomicAdd(&s_count, 1)] = key;
+    }
+    __syncthreads();
+    const int kept = s_count;
     auto put = [&](int j, uint64_t key) {
         const int64_t o = (int64_t)r * n_top + j;
         if (top_ids) top_ids[o] = key && !bad ? key_token(key) : -1;
         if (top_logprobs) top_logprobs[o] = key ? logp(key_logit(key)) : (bad ? nan : -INFINITY);
     };
-    for (int i0 = 0; i0 < count; i0 += kLogThreads) {
-        const uint64_t key = i0 + tid < count ? all[i0 + tid] : 0;
-        int place = 0;
-        for (int i = 0; i < count; ++i) place += all[i] > key ? 1 : 0;
-        if (key && place < n_top) put(place, key);
+    for (int k = tid; k < kept; k += kLogThreads) {
+        const uint64_t key = s_keys[k];
+        int place = 0;                               // the number of greater ones
+        for (int o = 0; o < kept; ++o) place += s_keys[o] > key ? 1 : 0;
+        if (place < n_top) put(place, key);
     }
-    for (int i = 0; i < count; ++i) found += all[i] != 0 ? 1 : 0;
-    for (int j = found + tid; j < n_top; j += kLogThreads) put(j, 0);
+    for (int j = kept + tid; j < n_top; j += kLogThreads) put(j, 0);
 }
 
 static int slices_of(const owl_logprob_desc &d)

@@ -121,6 +121,7 @@ def test_commit_quant_refuses():
     (dict(rows=0), B.OWL_ERR_INVALID_ARG), (dict(vocab=0), B.OWL_ERR_INVALID_ARG), (dict(row_stride=999), B.OWL_ERR_INVALID_ARG),
     (dict(scale=0.0), B.OWL_ERR_INVALID_ARG), (dict(scale=float("inf")), B.OWL_ERR_INVALID_ARG), (dict(scale=float("nan")), B.OWL_ERR_INVALID_ARG),
     (dict(n_given=-1), B.OWL_ERR_INVALID_ARG), (dict(n_top=-1), B.OWL_ERR_INVALID_ARG), (dict(n_given=65), B.OWL_ERR_UNSUPPORTED),
+    (dict(vocab=(1 << 20) + 1, row_stride=1 << 21), B.OWL_ERR_UNSUPPORTED),
     (dict(n_top=33), B.OWL_ERR_UNSUPPORTED), (dict(dtype=3), B.OWL_ERR_UNSUPPORTED),
 ])
 def test_logprobs_refuse_descriptors(over, code):
