@@ -99,6 +99,17 @@ def test_excluded_tokens_rows_without_any_and_what_is_no_number():
     assert int(c.status.item()) == B.OWL_DEV_BAD_LOGIT | B.OWL_DEV_BAD_TOKEN
 
 
+@pytest.mark.parametrize("dtype", [B.OWL_F32, B.OWL_BF16])
+@pytest.mark.parametrize("rows,vocab", [(300, 8185), (300, 8186), (300, 9000), (2, 32761), (2, 32762), (1, 1 << 20)])
+def test_rows_at_the_borders_between_one_launch_and_two(rows, vocab, dtype):
+    r = rng(vocab)
+    x = r.standard_normal((rows, vocab)).astype(np.float32)
+    x[-1] = np.sort(x[-1])                               # the greatest side by side
+    x[0, :] = -4.0
+    x[0, r.integers(0, vocab, 40)] = 3.0                 # few great ones, the rest equal
+    Call(x, r.integers(0, vocab, (rows, 2)).astype(np.int32), 32, dtype=dtype).run().check()
+
+
 def test_outputs_that_are_not_wanted():
     r = rng(3)
     x = r.standard_normal((3, 500)).astype(np.float32)
