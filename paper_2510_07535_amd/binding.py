@@ -459,19 +459,31 @@ def owl_verify_attn_ragged(desc: VerifyDesc, q, k_cache, v_cache, page_table, ct
 def owl_append_kv(desc: VerifyDesc, append: AppendDesc, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, page_table,
                   ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
     """q, k_new, v_new may be views of one fused projection: only their first elements and ``append``'s strides count."""
-    rc = lib().owl_append_kv(ctypes.byref(desc), ctypes.byref(append), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(inv_freq),
-                             _ptr(pos_ids), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(ctx_lens),
-                             _ptr(n_new_seq), _ptr(dev_status), _stream() if stream is None else stream)
-    _check(rc, "owl_append_kv")
+    rc = lib().owl_append_kv(
+        ctypes.byref(desc), ctypes.byref(append), None if q is None else q.data_ptr(), None if k_new is None else k_new.data_ptr(),
+        None if v_new is None else v_new.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+        None if pos_ids is None else pos_ids.data_ptr(), None if q_out is None else q_out.data_ptr(),
+        None if k_cache is None else k_cache.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
+        None if page_table is None else page_table.data_ptr(), None if ctx_lens is None else ctx_lens.data_ptr(),
+        None if n_new_seq is None else n_new_seq.data_ptr(), None if dev_status is None else dev_status.data_ptr(),
+        _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_append_kv")
 
 
 def owl_append_kv_quant(desc: VerifyDesc, append: AppendDesc, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale,
                         v_scale, page_table, ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
-    rc = lib().owl_append_kv_quant(ctypes.byref(desc), ctypes.byref(append), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(inv_freq),
-                                   _ptr(pos_ids), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale),
-                                   _ptr(page_table), _ptr(ctx_lens), _ptr(n_new_seq), _ptr(dev_status),
-                                   _stream() if stream is None else stream)
-    _check(rc, "owl_append_kv_quant")
+    rc = lib().owl_append_kv_quant(
+        ctypes.byref(desc), ctypes.byref(append), None if q is None else q.data_ptr(), None if k_new is None else k_new.data_ptr(),
+        None if v_new is None else v_new.data_ptr(), None if inv_freq is None else inv_freq.data_ptr(),
+        None if pos_ids is None else pos_ids.data_ptr(), None if q_out is None else q_out.data_ptr(),
+        None if k_cache is None else k_cache.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
+        None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
+        None if page_table is None else page_table.data_ptr(), None if ctx_lens is None else ctx_lens.data_ptr(),
+        None if n_new_seq is None else n_new_seq.data_ptr(), None if dev_status is None else dev_status.data_ptr(),
+        _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_append_kv_quant")
 
 
 def owl_verify_attn_quant_workspace_size(desc: VerifyDesc) -> int:
@@ -488,18 +500,28 @@ def owl_verify_attn_quant(desc: VerifyDesc, q, k_cache, v_cache, k_scale, v_scal
                           out, workspace, dev_status=None, stream: Optional[int] = None) -> None:
     """owl_verify_attn over a cache of 8-bit blocks: uint8 (or float8_e4m3fn) pools, uint8 scales [n_pool_pages][Hkv]."""
     rc = lib().owl_verify_attn_quant(
-        ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(page_table), _ptr(ctx_lens),
-        _ptr(tree_parent), _ptr(n_draft_seq), _ptr(out), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
-        _ptr(dev_status), _stream() if stream is None else stream)
-    _check(rc, "owl_verify_attn_quant")
+        ctypes.byref(desc), None if q is None else q.data_ptr(), None if k_cache is None else k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+        None if v_scale is None else v_scale.data_ptr(), None if page_table is None else page_table.data_ptr(),
+        None if ctx_lens is None else ctx_lens.data_ptr(), None if tree_parent is None else tree_parent.data_ptr(),
+        None if n_draft_seq is None else n_draft_seq.data_ptr(), None if out is None else out.data_ptr(),
+        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_verify_attn_quant")
 
 
 def owl_commit_kv_quant(desc: VerifyDesc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,
                         new_ctx_lens=None, dev_status=None, stream: Optional[int] = None) -> None:
-    rc = lib().owl_commit_kv_quant(ctypes.byref(desc), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(page_table),
-                                   _ptr(ctx_lens), _ptr(accepted), _ptr(n_accept), _ptr(new_ctx_lens), _ptr(dev_status),
-                                   _stream() if stream is None else stream)
-    _check(rc, "owl_commit_kv_quant")
+    rc = lib().owl_commit_kv_quant(
+        ctypes.byref(desc), None if k_cache is None else k_cache.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
+        None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
+        None if page_table is None else page_table.data_ptr(), None if ctx_lens is None else ctx_lens.data_ptr(),
+        None if accepted is None else accepted.data_ptr(), None if n_accept is None else n_accept.data_ptr(),
+        None if new_ctx_lens is None else new_ctx_lens.data_ptr(), None if dev_status is None else dev_status.data_ptr(),
+        _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_commit_kv_quant")
 
 
 def owl_token_logprobs_workspace_size(desc: LogprobDesc) -> int:
@@ -510,10 +532,14 @@ def owl_token_logprobs_workspace_size(desc: LogprobDesc) -> int:
 
 def owl_token_logprobs(desc: LogprobDesc, logits, tokens, logprob, entropy, top_ids, top_logprobs, workspace, dev_status=None,
                        stream: Optional[int] = None) -> None:
-    rc = lib().owl_token_logprobs(ctypes.byref(desc), _ptr(logits), _ptr(tokens), _ptr(logprob), _ptr(entropy), _ptr(top_ids),
-                                  _ptr(top_logprobs), _ptr(workspace), 0 if workspace is None else workspace.nbytes,
-                                  _ptr(dev_status), _stream() if stream is None else stream)
-    _check(rc, "owl_token_logprobs")
+    rc = lib().owl_token_logprobs(
+        ctypes.byref(desc), None if logits is None else logits.data_ptr(), None if tokens is None else tokens.data_ptr(),
+        None if logprob is None else logprob.data_ptr(), None if entropy is None else entropy.data_ptr(),
+        None if top_ids is None else top_ids.data_ptr(), None if top_logprobs is None else top_logprobs.data_ptr(),
+        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_token_logprobs")
 
 
 def owl_mfma_probe(src, iters: int, sink, n_workgroups: int, stream: Optional[int] = None, clock_ghz=None) -> None:
