@@ -15,10 +15,10 @@ typedef float a_f32x2 __attribute__((ext_vector_type(2)));
 // key by half a bf16 step; t * inv_freq is exact in 64 bits.  What the turned channels are rounded to is then the
 // number nearest to the formula's, but for one in some 10^9.
 // ---------------------------------------------------------------------------
-// sin a and cos a to about 1e-16: the nearest multiple k of pi/2 is taken off (pi/2 in two parts; with fused products the
+// scale * sin a and scale * cos a, to about 1e-16 of it: the nearest multiple k of pi/2 is taken off (pi/2 in two parts; with fused products the
 // rest is exact to its last place for |k| < 2^52), and on the rest, at most pi/4, the Taylor series end where the next term
 // is below 5e-17.
-__device__ __forceinline__ double2 cos_sin(double a)
+__device__ __forceinline__ double2 cos_sin(double a, double scale)
 {
     const double k = __builtin_rint(a * 0.63661977236758134308);
     double r = __builtin_fma(-k, 1.57079632679489655800, a);
@@ -41,7 +41,7 @@ __device__ __forceinline__ double2 cos_sin(double a)
     c = __builtin_fma(c, z, -0.5);
     c = __builtin_fma(c, z, 1.0);
     const int quarter = (int)(k - 4.0 * __builtin_floor(k * 0.25));
-    const double x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+    const double x = (quarter & 1 ? s : c) * scale, y = (quarter & 1 ? c : s) * scale;
     return make_double2(quarter == 1 || quarter == 2 ? -x : x, quarter >= 2 ? -y : y);
 }
 
@@ -124,9 +124,9 @@ __device__ __forceinline__ int2 item_at(int i, int rot_dim)
     return make_int2(E * i, rot_dim / 2 + E * i);
 }
 
-// Turns an item.  The cosine and sine of frequency E i + e are at cs[e * step].
+// Turns an item.  The cosine and sine of frequency E i + e, times the scale, are at cs[e * step].
 template <typename T, bool kPairs>
-__device__ __forceinline__ void turn(Piece<T> &a, Piece<T> &b, const double2 *cs, int step, double scale)
+__device__ __forceinline__ void turn(Piece<T> &a, Piece<T> &b, const double2 *cs, int step)
 {
     constexpr int E = Piece<T>::E;
 #pragma unroll
@@ -135,7 +135,7 @@ __device__ __forceinline__ void turn(Piece<T> &a, Piece<T> &b, const double2 *cs
         float &x = kPairs ? (2 * e < E ? a.v[(2 * e) % E] : b.v[(2 * e) % E]) : a.v[e];
         float &y = kPairs ? (2 * e < E ? a.v[(2 * e + 1) % E] : b.v[(2 * e + 1) % E]) : b.v[e];
         const double xd = x, yd = y;
-        const double p = (xd * w.x - yd * w.y) * scale, q = (yd * w.x + xd * w.y) * scale;
+        const double p = xd * w.x - yd * w.y, q = yd * w.x + xd * w.y;
         x = std::is_same<T, float>::value ? (float)p : to_odd(p);
         y = std::is_same<T, float>::value ? (float)q : to_odd(q);
     }
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
     const int turned = p.rot_dim / (2 * E);                  // items of a head that are turned
     if (tid < p.rot_dim / 2) {
         const int t = p.pos_ids ? p.pos_ids[token] : at;
-        s_cs[tid % E * turned + tid / E] = cos_sin((double)t * (double)p.inv_freq[tid]);
+        s_cs[tid % E * turned + tid / E] = cos_sin((double)t * (double)p.inv_freq[tid], (double)p.rot_scale);
     }
     __syncthreads();
     const int q_heads = p.q ? p.Hq : 0, heads = q_heads + 2 * p.Hkv;
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
         uint4 x = load16(from + c.x * ES), y = load16(from + c.y * ES);
         if (rotate) {
             Piece<T> a = unpack<T>(x), z = unpack<T>(y);
-            turn<T, kPairs>(a, z, s_cs + item, turned, (double)p.rot_scale);
+            turn<T, kPairs>(a, z, s_cs + item, turned);
             x = pack<T>(a);
             y = pack<T>(z);
         }
@@ -277,7 +277,12 @@ __device__ __forceinline__ uint32_t greatest(const float *v)
 
 // ---------------------------------------------------------------------------
 // Append to 8-bit blocks: one workgroup per (16-token block, KV head, sequence).  Its first half takes the block of K, its second that
-// of V, an item a thread; then all of it turns the query heads of the group.
+// of V, an item a thread; then all of it turns the query heads of the group.  A block's scale depends on all its rows, so the
+// old ones are read again and the block is written whole; positions that lie side by side cost each block once.
+// Long chunks are bound by memory: 4 prompts' chunks of 2501 tokens, 389 MB, 82 us (4.8 TB/s, what a large copy reaches).  Trees are
+// bound by one workgroup's chain, lengths -> page -> old block, angles and products in 64 bits -> greatest magnitude -> block: 16
+// sequences with up to 26 tokens 8.0 us in a graph (8.8 with the queries read behind the block and angles one after the other; 8.4 with
+// 512 threads, with which chunks take 87.7).
 // ---------------------------------------------------------------------------
 template <typename T, int D, bool kPairs>
 __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const AppendArgs p)
@@ -296,11 +301,17 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     const int page = good ? append_page(p, b, block, teller) : -1;
     const int half = p.rot_dim / 2, turned = p.rot_dim / (2 * E);
     if (tid < 2) s_big[tid] = 0;
-    for (int id = tid; id < kPage * half; id += kAppendThreads) {
-        const int slot = id / half, f = id - slot * half, i = first + slot;
-        if (i >= 0 && i < n_b) {
-            const int t = p.pos_ids ? p.pos_ids[(int64_t)b * p.n + i] : L + i;
-            s_cs[slot * (D / 2 + 8) + f % E * turned + f / E] = cos_sin((double)t * (double)p.inv_freq[f]);
+    // a thread a frequency, of every fourth (eighth) token: the chains of its angles run side by side
+    constexpr int kAtOnce = kAppendThreads / (D / 2), kAngles = kPage / kAtOnce;
+    const int f = tid % (D / 2);
+    double angle[kAngles];
+    {
+        const double freq = f < half ? (double)p.inv_freq[f] : 0.0;
+#pragma unroll
+        for (int k = 0; k < kAngles; ++k) {
+            const int i = first + tid / (D / 2) + k * kAtOnce;
+            const int t = p.pos_ids && i >= 0 && i < n_b ? p.pos_ids[(int64_t)b * p.n + i] : L + i;
+            angle[k] = (double)t * freq;
         }
     }
     // this thread's 16 numbers of the block
@@ -322,12 +333,54 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
         y = make_uint4(w.x, w.y, 0, 0);
         old_scale = __builtin_bit_cast(float, (uint32_t)*scale_at << 23);
     }
+    // and its first two items of the queries: all that is read is asked for before the angles are formed
+    const int group = p.Hq / p.Hkv, q_items = p.q ? kPage * group * kItems : 0;
+    struct Query {
+        int item, slot;                                      // slot -1: none
+        int64_t row;
+        uint4 x, y;
+    };
+    auto query = [&](int id) -> Query {
+        Query r;
+        r.item = id % kItems;
+        const int rest = id / kItems, s = (int)(((float)rest + 0.5f) * __builtin_amdgcn_rcpf((float)group));     // rest / group, exactly
+        const int tok = first + s;
+        const bool is = id < q_items && tok >= 0 && tok < n_b;
+        r.slot = is ? s : -1;
+        if (!is) return r;
+        const int head = g * group + rest - s * group;
+        const int64_t token = (int64_t)b * p.n + tok;
+        const int2 at = item_at<E, kPairs>(r.item, p.rot_dim);
+        r.row = token * p.Hq + head;
+        const unsigned char *from = p.q + token * p.q_stride + head * (D * ES);
+        r.x = load16(from + at.x * ES);
+        r.y = load16(from + at.y * ES);
+        return r;
+    };
+    auto answer = [&](const Query &r) {
+        if (r.slot < 0) return;
+        const int2 at = item_at<E, kPairs>(r.item, p.rot_dim);
+        uint4 u = r.x, w = r.y;
+        if (r.item < turned) {
+            Piece<T> a = unpack<T>(u), z = unpack<T>(w);
+            turn<T, kPairs>(a, z, s_cs + r.slot * (D / 2 + 8) + r.item, turned);
+            u = pack<T>(a);
+            w = pack<T>(z);
+        }
+        unsigned char *out = p.q_out + r.row * (D * ES);
+        store16(out + at.x * ES, u);
+        store16(out + at.y * ES, w);
+    };
+    Query q0 = query(tid), q1 = query(tid + kAppendThreads);
+#pragma unroll
+    for (int k = 0; k < kAngles; ++k)
+        if (f < half) s_cs[(tid / (D / 2) + k * kAtOnce) * (D / 2 + 8) + f % E * turned + f / E] = cos_sin(angle[k], (double)p.rot_scale);
     __syncthreads();
     float v[2 * E] = {};
     if (mine && i >= 0) {
         Piece<T> a = unpack<T>(x), z = unpack<T>(y);
         if (tensor == 0 && item < turned) {
-            turn<T, kPairs>(a, z, s_cs + slot * (D / 2 + 8) + item, turned, (double)p.rot_scale);
+            turn<T, kPairs>(a, z, s_cs + slot * (D / 2 + 8) + item, turned);
             a = unpack<T>(pack<T>(a));                       // what a 16-bit cache would hold
             z = unpack<T>(pack<T>(z));
         }
@@ -346,6 +399,12 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     for (int e = 0; e < 2 * E; ++e) v[e] = admit<T>(v[e]);
     const int big = wave_max((int)greatest<2 * E>(v));
     if ((tid & 63) == 0) atomicMax(&s_big[tensor], (uint32_t)big);
+    for (int id = tid; id < q_items; id += 2 * kAppendThreads) {
+        answer(q0);
+        answer(q1);
+        q0 = query(id + 2 * kAppendThreads);
+        q1 = query(id + 3 * kAppendThreads);
+    }
     __syncthreads();
     if (mine) {
         const int e = block_exponent<T>(s_big[tensor]);
@@ -353,25 +412,6 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
         *reinterpret_cast<uint2 *>(to + c.x) = make_uint2(narrow4(v, scale), narrow4(v + 4, scale));
         *reinterpret_cast<uint2 *>(to + c.y) = make_uint2(narrow4(v + 8, scale), narrow4(v + 12, scale));
         if (own == 0) *scale_at = (uint8_t)(e + 127);
-    }
-    if (!p.q) return;
-    const int group = p.Hq / p.Hkv;
-    for (int id = tid; id < kPage * group * kItems; id += kAppendThreads) {
-        const int it = id % kItems, rest = id / kItems, s = rest / group, head = g * group + rest - s * group, tok = first + s;
-        if (tok < 0 || tok >= n_b) continue;
-        const int2 at = item_at<E, kPairs>(it, p.rot_dim);
-        const int64_t token = (int64_t)b * p.n + tok;
-        const unsigned char *from = p.q + token * p.q_stride + head * (D * ES);
-        unsigned char *out = p.q_out + (token * p.Hq + head) * (D * ES);
-        uint4 u = load16(from + at.x * ES), w = load16(from + at.y * ES);
-        if (it < turned) {
-            Piece<T> a = unpack<T>(u), z = unpack<T>(w);
-            turn<T, kPairs>(a, z, s_cs + s * (D / 2 + 8) + it, turned, (double)p.rot_scale);
-            u = pack<T>(a);
-            w = pack<T>(z);
-        }
-        store16(out + at.x * ES, u);
-        store16(out + at.y * ES, w);
     }
 }
 
