@@ -102,11 +102,13 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // groups instead, each re-reading the split from its XCD's L2.
     int tpw, wr, wk, rgs, group_tiles;
     // Over 8-bit blocks few tiles go to wavefronts with keys of their own, two tiles a row group (owl_splitkv_few.hip), many to
-    // the shared ring.  us, ring -> own keys, 8 KV heads, head_dim 128: 64K context, 1 tile 40.5 -> 27.3, 3 44.0 -> 39.8, 4 44.8 ->
-    // 40.8, 5 59.1 -> 51.5, 6 60.6 -> 52.0, 7 61.7 -> 59.8, 8 62.8 -> 60.3, and 15 in groups of two 84.5 -> 99.7; 8 tiles of 1 KV head
-    // 22.0 -> 17.6; 16 sequences of 8K-64K, 1 tile 309 -> 213, 3 331 -> 296, 4 336 -> 303, 5 469 -> 421, but 7 399 -> 499 (four groups
-    // read each key from L2, and in a batch nothing else is short of time).
-    const bool few = quant && RT <= (d->batch == 1 ? 8 : 6);
+    // the shared ring.  us, ring -> own keys, 8 KV heads, head_dim 128, bf16: 64K context, 1 tile 39.0 -> 27.7, 3 40.9 -> 39.5, 4 41.9 -> 40.9, 5
+    // 51.3 -> 51.1, 6 51.6 -> 51.5, 7 52.7 -> 59.6, 8 55.1 -> 60.7; 16 sequences of 8K-64K, 1 tile 302 -> 211, 3 312 -> 296, 4 331 -> 298, 5 389 ->
+    // 425, 6 410 -> 426, 7 408 -> 507 (more groups read each key from L2 and widen it again).  Short streams gain longer: 8 tiles of 1 KV
+    // head 20.8 -> 17.6, of 2 24.5 -> 23.1, of 4 34.1 -> 35.0.  So does fp16, whose ring guards its references: 5 tiles 59.1 -> 51.4, 7 63.3 ->
+    // 59.1, in the batch 5 480 -> 421, 6 485 -> 430, 7 438 -> 500.
+    const bool lone = d->batch == 1;
+    const bool few = quant && RT <= (d->qkv_dtype == OWL_F16 ? (lone ? 8 : 6) : !lone ? 4 : d->n_kv_heads > 2 ? 6 : 8);
     if (few) {
         rgs = (RT + 1) / 2;
         group_tiles = (RT + rgs - 1) / rgs;

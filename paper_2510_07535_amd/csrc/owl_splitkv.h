@@ -41,15 +41,10 @@
 // one more channel tile whose V^T operand is all ones, so it is summed from the
 // very P values (after rounding to bf16) that weigh V.
 //
-// A cache of 8-bit blocks (kQuant) goes through the same loops.  Its bytes travel as they are, half the
-// traffic and twice the stages in the ring, the scale of a page with them, and a wavefront turns the fragments
-// it has read from LDS into 16 bits, scale applied: a power of two times a number of three mantissa bits, exact in
-// bf16 and, inside its range, in fp16.  The results are those of a 16-bit cache that holds the same numbers.
-// A 16-byte read of K holds channels 16 p .. 16 p + 15 of a key: its halves are two k-steps (the order of the
-// contraction index is free), and the query fragments take the same order.  V^T fragments come from
-// ds_read_b64_tr_b8: in a block of 16 lanes, lane i receives element i % 8 of the 8 bytes addressed by lanes
-// 2e + i/8 (e = 0..7); with lane 2e + c pointing at channels 8c .. 8c + 7 of key e, lane i ends up with
-// channel i of eight keys: one read for a fragment.
+// A cache of 8-bit blocks (kQuant) goes through the same loops.  Its bytes travel as they are, half the traffic, each wavefront's
+// page and its scale into a part of LDS of its own, and a stage ahead of its use the wavefront turns its page into 16 bits,
+// scale applied, and puts it into the ring: a power of two times a number of three mantissa bits, exact in bf16 and, inside its
+// range, in fp16.  The results are those of a 16-bit cache that holds the same numbers.
 //
 // Visibility (Sec. 3.2.2, Decode Stage): every row sees the whole prefix; among
 // the drafts, row (i, .) sees node j iff j is on i's root path, i included.
@@ -188,14 +183,6 @@ __device__ __forceinline__ uint2 lds_read_tr16(const unsigned char *p)
     return __builtin_bit_cast(uint2, v);
 }
 
-// Transposing 64-bit LDS read of bytes (likewise).
-__device__ __forceinline__ uint2 lds_read_tr8(const unsigned char *p)
-{
-    typedef int i32x2 __attribute__((ext_vector_type(2)));
-    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3))) *)(p));
-    return __builtin_bit_cast(uint2, v);
-}
-
 // f(integral_constant<int, B>) ... f(integral_constant<int, E-1>), unrolled at compile time.
 template <int B, int E, typename F>
 __device__ __forceinline__ void static_for(F &&f)
@@ -211,38 +198,32 @@ template <typename T, int D, int TPW, int WR, int WK, bool kQuant>
 struct Geo {
     static constexpr bool kF32 = std::is_same<T, float>::value;
     static constexpr int ES = sizeof(T);
-    static constexpr int CB = kQuant ? 1 : ES;          // bytes of a cached element
     static constexpr int KSTEPS = 2;                    // 32-key steps per stage
     static constexpr int SK = 32 * KSTEPS;              // keys per stage: 4 pages x 2 tensors = 8 waves
-    static constexpr int ROWB = D * CB;                 // bytes of one key row
+    static constexpr int ROWB = D * ES;                 // bytes of one key row
     static constexpr int PPR = ROWB / 16;               // 16-byte pieces per row
-    static constexpr int RPI = 1024 / ROWB;             // key rows per DMA instruction
-    static constexpr int DMAS = kPage / RPI;            // DMA instructions per page of one tensor
+    static constexpr int QRPI = 1024 / ROWB, QDMAS = kPage / QRPI;      // rows per DMA instruction, instructions per page: of queries,
+    static constexpr int CB = kQuant ? 1 : ES, CROWB = D * CB, CPPR = CROWB / 16;   // and of what is cached, of CB bytes a number
+    static constexpr int RPI = 1024 / CROWB;
+    static constexpr int DMAS = kPage / RPI;
     static constexpr int LPS = DMAS + (kQuant ? 1 : 0); // loads in flight per wave and stage: the page and its scale
     static constexpr int NT = D / 16;                   // channel tiles of O^T
     static constexpr int STAGE = SK * ROWB;             // bytes per tensor per stage
-    static constexpr int NS = kQuant ? 8 : ((8 * STAGE <= 131072) ? 4 : ((6 * STAGE <= 131072) ? 3 : 2));
+    static constexpr int NS = kQuant ? 3 : ((8 * STAGE <= 131072) ? 4 : ((6 * STAGE <= 131072) ? 3 : 2));
     static constexpr int VREG = NS * STAGE;             // LDS ring: K stages at [0, VREG), V stages behind them
     static constexpr int QREGS = kF32 ? D / 4 : D / 32; // Q fragment slots per tile
-    static constexpr int QROWB = D * ES;                // a query row: its bytes, pieces, rows and instructions of a DMA
-    static constexpr int QPPR = QROWB / 16, QRPI = 1024 / QROWB, QDMAS = kPage / QRPI;
-    static constexpr int QSLOTS = 4 * kPage * QROWB / STAGE;    // ring slots that one tile of every wavefront takes
     static constexpr int KSWZ = (PPR - 1) & 15;         // K rows: piece ^= key & KSWZ
     static constexpr int VSWM = PPR >= 16 ? 7 : PPR / 2 - 1;   // V rows: piece ^= (key & VSWM) << 1
-    static constexpr int QSWZ = (QPPR - 1) & 15;
-    static constexpr size_t PAGES = (size_t)NS * 2 * STAGE;           // behind the ring: page list, ancestor sets, parents, votes
+    // 8-bit blocks: stages as they are cached, behind the ring
+    static constexpr int NR = kQuant ? 3 * 128 / D : 0, RAW = NS * 2 * STAGE, RAW_PAGE = kPage * CROWB, RAW_STAGE = kWaves * RAW_PAGE;
+    static constexpr size_t PAGES = (size_t)RAW + NR * RAW_STAGE;     // then: page list, ancestor sets, parents, votes
     static constexpr size_t ANC = PAGES + kMaxPiecePages * 4, PARENT = ANC + 64 * 8, ANY = PARENT + 64 * 4;
     static constexpr size_t SCALES = ANY + 2 * kWaves * 4;            // 8-bit blocks: the scale byte of each wavefront's page, for each stage
-    static constexpr size_t LDS = SCALES + (kQuant ? NS * kWaves * 4 : 0);
+    static constexpr size_t LDS = SCALES + NR * kWaves * 4;
     static_assert(WR * WK == kWaves && (WK == 1 || WK == 2), "eight wavefronts per workgroup");
-    static_assert(NS * LPS < 64, "loads in flight must fit vmcnt");
-    static_assert((WK - 1) * WR * TPW * (NT * 1024 + 512) <= NS * 2 * STAGE,
+    static_assert((kQuant ? NR + 1 : NS) * LPS < 64, "loads in flight must fit vmcnt");
+    static_assert((WK - 1) * WR * TPW * (NT * 1024 + 512) <= NS * 2 * STAGE + NR * RAW_STAGE,
                   "cross-wave merge buffer must fit in the stage ring");
-    // 8-bit blocks: the piece in which piece 0 of a row sits (XOR), so that the fragment reads meet no bank twice.  The 16 rows
-    // that 16 lanes read at a time are, of K, those of a page, and of V slots 0-7 (or 8-15) of two pages; 256 / ROWB rows
-    // share a round of the banks.
-    static constexpr int k_turn(int slot) { return slot / (256 / ROWB) & (PPR - 1); }
-    static constexpr int v_turn(int slot, int page) { return (slot / (256 / ROWB) & (PPR / 2 - 1)) | (page & 1) * (PPR / 2); }
 };
 
 // One piece of work: the stages of sequence b between two token positions.
@@ -332,7 +313,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
 {
     using GEO = Geo<T, D, TPW, WR, WK, kQuant>;
     constexpr bool kF32 = GEO::kF32;
-    constexpr int ES = GEO::ES, CB = GEO::CB, DMAS = GEO::DMAS, QROWB = GEO::QROWB, KSTEPS = GEO::KSTEPS, SK = GEO::SK, ROWB = GEO::ROWB;
+    constexpr int ES = GEO::ES, CB = GEO::CB, DMAS = GEO::DMAS, KSTEPS = GEO::KSTEPS, SK = GEO::SK, ROWB = GEO::ROWB;
     constexpr int PPR = GEO::PPR, NT = GEO::NT, STAGE = GEO::STAGE, NS = GEO::NS;
     constexpr int RPI = GEO::RPI, LPS = GEO::LPS, QREGS = GEO::QREGS;
     constexpr int KSWZ = GEO::KSWZ, VSWM = GEO::VSWM, VREG = GEO::VREG;
@@ -374,7 +355,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     const float inv_g = __builtin_amdgcn_rcpf((float)heads);
     auto node_of = [&](int row) -> int { return (int)(((float)row + 0.5f) * inv_g); };
     const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * ES;
-    auto row_offset = [&](int row) -> int64_t { return ((int64_t)node_of(row) * (p.Hq - p.G) + row) * QROWB; };
+    auto row_offset = [&](int row) -> int64_t { return ((int64_t)node_of(row) * (p.Hq - p.G) + row) * ROWB; };
     uint4 qf[TPW][KQ];
     float qs[TPW][kF32 ? QREGS : 1];
     int irow[TPW];
@@ -433,7 +414,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     const int ld_tensor = wave >> 2, ld_page = wave & 3;
     const unsigned char *ld_base = static_cast<const unsigned char *>(ld_tensor ? p.v : p.k);
     const int last_pgx = (pos1 - 1 - pos0) >> 4, last_slot = (pos1 - 1) & (kPage - 1);
-    const int ld_piece = lane % PPR, ld_row = lane / PPR;
+    const int ld_piece = lane % GEO::CPPR, ld_row = lane / GEO::CPPR;
     const int64_t head_off = (int64_t)g * p.stride_head * CB;
     const int64_t tok_bytes = p.stride_token * CB;
     // (Held in their registers: fp16's arguments are in memory, and left to the compiler every stage of its loops loaded the
@@ -447,19 +428,18 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // (wave-uniform, kept in scalar registers) changes from stage to stage.
     constexpr bool kKeepLdOff = TPW <= 2;            // three tiles per wave: no registers to spare, recompute
     auto ld_swizzle = [&](int row) -> int {
-        if constexpr (kQuant) return ld_tensor ? GEO::v_turn(row, ld_page) : GEO::k_turn(row);
         return ld_tensor ? ((row & VSWM) << 1) : (row & KSWZ);
     };
     auto ld_off_of = [&](int it) -> uint32_t {
         const int row = it * RPI + ld_row;
-        const int swz = ld_swizzle(row);
+        const int swz = kQuant ? 0 : ld_swizzle(row);
         return (uint32_t)(row * tok_bytes) + (uint32_t)((ld_piece ^ swz) << 4);
     };
     uint32_t ld_off[DMAS];
 #pragma unroll
     for (int it = 0; it < DMAS; ++it) ld_off[it] = kKeepLdOff ? ld_off_of(it) : 0u;
     const bool ld_off_ok = tok_bytes * kPage < ((int64_t)1 << 31);
-    const uint32_t ld_lds = lds0 + ld_tensor * VREG + ld_page * kPage * ROWB;
+    const uint32_t ld_lds = lds0 + (kQuant ? GEO::RAW + wave * GEO::RAW_PAGE : ld_tensor * VREG + ld_page * kPage * ROWB);
 
     // page id of this wave's page of stage s (to be handed to issue_stage; reading it
     // ahead of the stage barrier takes the LDS round trip off the issue path)
@@ -470,16 +450,16 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                      __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)GEO::SCALES + (buf * kWaves + wave) * 4));
     };
     auto issue_stage_pg = [&](int s, int pg_lane) {
-        const int buf = s % NS;
+        const int buf = s % (kQuant ? GEO::NR : NS);
         const int pgx_raw = s * (SK / kPage) + ld_page;
-        const uint32_t lds_dst = ld_lds + buf * STAGE;
+        const uint32_t lds_dst = ld_lds + buf * (kQuant ? GEO::RAW_STAGE : STAGE);
         if (pgx_raw < last_pgx && ld_off_ok) {           // uniform over the wave
             const int64_t pg = __builtin_amdgcn_readfirstlane(pg_lane);
             const uint64_t sbase = uniform64((uint64_t)(uintptr_t)ld_base + (uint64_t)(pg * page_bytes + head_off));
 #pragma unroll
             for (int it = 0; it < DMAS; ++it)
                 dma16s(sbase, kKeepLdOff ? ld_off[it] : ld_off_of(it),
-                       __builtin_amdgcn_readfirstlane(lds_dst + it * RPI * ROWB));
+                       __builtin_amdgcn_readfirstlane(lds_dst + it * RPI * GEO::CROWB));
             issue_scale(buf, pg);
             return;
         }
@@ -489,9 +469,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         for (int it = 0; it < DMAS; ++it) {
             const int row = it * RPI + ld_row;
             const int64_t off = base + min(row, slot_max) * tok_bytes;
-            const int swz = ld_swizzle(row);
+            const int swz = kQuant ? 0 : ld_swizzle(row);
             dma16<true>(ld_base + off + ((ld_piece ^ swz) << 4),
-                  __builtin_amdgcn_readfirstlane(lds_dst + it * RPI * ROWB));
+                  __builtin_amdgcn_readfirstlane(lds_dst + it * RPI * GEO::CROWB));
         }
         issue_scale(buf, __builtin_amdgcn_readfirstlane(pg_lane));
     };
@@ -502,9 +482,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // there each wavefront picks its own fragments.  (Loaded straight into registers they took 2 us for
     // 20 row tiles, as 64-byte pieces of 16 rows per instruction, and the compiler, which does not see the
     // ring's transfers in the wait counter, drained the whole ring before it used them.)
-    constexpr int kQSlot0 = NS - TPW * GEO::QSLOTS;  // first ring slot the queries occupy
+    constexpr int kQSlot0 = NS - TPW;  // first ring slot the queries occupy
     auto q_lds = [&](int t) -> uint32_t {            // offset of this wavefront's tile t in the ring
-        return (uint32_t)((kQSlot0 + t * GEO::QSLOTS) * STAGE + (wave & 3) * (kPage * QROWB) + (wave >> 2) * VREG);
+        return (uint32_t)((kQSlot0 + t) * STAGE + (wave & 3) * (kPage * ROWB) + (wave >> 2) * VREG);
     };
     // Every worker of a head reads the same rows, so they stay in the caches, except where one worker takes the whole
     // sequence (non-temporal against cached, us: 24 rows, 8 heads, 5K tokens 14.0 -> 13.2, 320 rows, 1 head, 10K 15.3 -> 14.3,
@@ -519,9 +499,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                 const int row0 = (rg * p.group_tiles + t * WR + wr) * kRowTile;
 #pragma unroll
                 for (int it = 0; it < GEO::QDMAS; ++it) {
-                    const int slot = it * GEO::QRPI + lane / GEO::QPPR;
-                    const unsigned char *src = q_head + row_offset(min(row0 + slot, p.R - 1)) + ((lane % GEO::QPPR ^ (slot & GEO::QSWZ)) << 4);
-                    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + q_lds(t) + it * GEO::QRPI * QROWB);
+                    const int slot = it * GEO::QRPI + lane / PPR;
+                    const unsigned char *src = q_head + row_offset(min(row0 + slot, p.R - 1)) + ((lane % PPR ^ (slot & KSWZ)) << 4);
+                    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds0 + q_lds(t) + it * GEO::QRPI * ROWB);
                     if (once) dma16<true>(src, dst);
                     else dma16<false>(src, dst);
                 }
@@ -534,14 +514,12 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             for (int t = 0; t < TPW; ++t)
 #pragma unroll
                 for (int kk = 0; kk < KQ; ++kk) {
-                    // 8-bit blocks: channels 64 (kk / 2) + 16 quad + 8 (kk % 2) .. + 7, as a 16-byte read of K brings them
-                    const int piece = kQuant ? 8 * (kk / 2) + 2 * qd + kk % 2 : 4 * kk + qd;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(smem + q_lds(t) + j * QROWB + ((piece ^ (j & GEO::QSWZ)) << 4));
+                    const uint4 x = *reinterpret_cast<const uint4 *>(smem + q_lds(t) + j * ROWB + (((4 * kk + qd) ^ (j & KSWZ)) << 4));
                     qf[t][kk] = irow[t] >= 0 ? x : make_uint4(0, 0, 0, 0);
                 }
         }
     };
-    static_assert(kF32 || (kQSlot0 > 0 && 4 * kPage * QROWB == GEO::QSLOTS * STAGE), "the queries leave at least one ring slot to the first stage");
+    static_assert(kF32 || (kQSlot0 >= (kQuant ? 0 : 1) && 4 * kPage * ROWB == STAGE), "the queries leave at least one ring slot to the first stage");
 
     f32x4 O[TPW][NT + 1];
     float m[TPW];
@@ -561,30 +539,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     const int v_swz = (v_key0 & VSWM) << 1;
     const int v_lane_off = v_key0 * ROWB + (v_c & 1) * 8;
 
-    // 8-bit blocks: the scales of the two pages of a step, of K (tensor 0) or V (1); `step` is s * KSTEPS + ks for step ks of
-    // stage s, or of any stage in the same ring slot
-    auto load_scales = [&](int step, int tensor) -> float2 {
-        if constexpr (kQuant) {
-            const uint2 e = *reinterpret_cast<const uint2 *>(smem + GEO::SCALES + step / KSTEPS % NS * (kWaves * 4) + step % KSTEPS * 8 + tensor * 16);
-            return make_float2(__builtin_bit_cast(float, e.x << 23), __builtin_bit_cast(float, e.y << 23));
-        } else {
-            return make_float2(0.f, 0.f);
-        }
-    };
     // ---- K fragments of one 32-key step ----
-    auto load_k_frags = [&](const unsigned char *Kb, [[maybe_unused]] float2 scales, uint4 (&kf)[2][KQ]) {
-        if constexpr (kQuant) {
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                const float scale = kt ? scales.y : scales.x;
-#pragma unroll
-                for (int c = 0; c < KQ / 2; ++c) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(Kb + (kt * 16 + j) * ROWB + (((4 * c + qd) ^ GEO::k_turn(j)) << 4));
-                    kf[kt][2 * c] = widen8<T>(make_uint2(x.x, x.y), scale, scale);
-                    kf[kt][2 * c + 1] = widen8<T>(make_uint2(x.z, x.w), scale, scale);
-                }
-            }
-        } else if constexpr (!kF32) {
+    auto load_k_frags = [&](const unsigned char *Kb, uint4 (&kf)[2][KQ]) {
+        if constexpr (!kF32) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
                 const int key = kt * 16 + j;
@@ -595,24 +552,12 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             }
         }
     };
-    // ---- V^T fragment of channel tile u for the 32 keys of a step, as it is cached, and in 16 bits ----
-    using VRaw = typename std::conditional<kQuant, uint2, uint4>::type;
-    auto load_v_frag = [&](const unsigned char *Vb, int u) -> VRaw {
-        if constexpr (kQuant) {
-            // lane 2e + c of block `quad`: key 4 quad + e of the first page, from e = 4 on 4 quad + e - 4 of the second, as the
-            // scores lie; channels 16 u + 8 c .. +7
-            const int slot = 4 * qd + ((j >> 1) & 3), page = j >> 3;
-            return lds_read_tr8(Vb + (page * kPage + slot) * ROWB + ((u ^ GEO::v_turn(slot, page)) << 4) + (j & 1) * 8);
-        } else {
-            const unsigned char *a = Vb + v_lane_off + ((((2 * u) ^ v_swz) | (v_c >> 1)) << 4);
-            const uint2 lo = lds_read_tr16(a);
-            const uint2 hi = lds_read_tr16(a + 16 * ROWB);
-            return make_uint4(lo.x, lo.y, hi.x, hi.y);
-        }
-    };
-    auto wide_v = [&](const VRaw &v, [[maybe_unused]] float2 scales) -> uint4 {
-        if constexpr (kQuant) return widen8<T>(v, scales.x, scales.y);
-        else return v;
+    // ---- V^T fragment of channel tile u for the 32 keys of a step ----
+    auto load_v_frag = [&](const unsigned char *Vb, int u) -> uint4 {
+        const unsigned char *a = Vb + v_lane_off + ((((2 * u) ^ v_swz) | (v_c >> 1)) << 4);
+        const uint2 lo = lds_read_tr16(a);
+        const uint2 hi = lds_read_tr16(a + 16 * ROWB);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
     };
 
     // ---- fast step: no mask, fixed reference m, accumulators touched by MFMA only ----
@@ -626,8 +571,8 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // A step is cut in two: scores + softmax -> P (fast_sx), and O += V^T P with
     // the V^T fragments already in registers (fast_pv), so that the stage loop
     // can put a barrier between them.
-    auto fast_sx = [&](const unsigned char *Kb, const unsigned char *Vb, int step, uint4 (&pf)[TPW], VRaw (&vf)[NT], float2 &vs, auto ntag, auto gtag,
-                       [[maybe_unused]] float room) {
+    auto fast_sx = [&](const unsigned char *Kb, const unsigned char *Vb, uint4 (&pf)[TPW], uint4 (&vf)[NT],
+                       auto ntag, auto gtag, [[maybe_unused]] float room) {
         constexpr int NA = decltype(ntag)::value;    // tiles this wave really owns
         constexpr bool kGuarded = decltype(gtag)::value;
         // One tile a wavefront: half of the V^T fragments are asked for behind the scores, so that they arrive while P is
@@ -643,8 +588,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             // gaps of the chain with its PV MFMAs (13 % fewer cycles in the three-tile loop).
             __builtin_amdgcn_s_setprio(1);
             uint4 kf[2][KQ];
-            load_k_frags(Kb, load_scales(step, 0), kf);
-            vs = load_scales(step, 1);
+            load_k_frags(Kb, kf);
 #pragma unroll
             for (int t = 0; t < NA; ++t) {
                 f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
@@ -689,16 +633,15 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             for (int u = kEarlyV ? NT / 2 : 0; u < NT; ++u) vf[u] = load_v_frag(Vb, u);
         }
     };
-    auto fast_pv = [&](const uint4 (&pf)[TPW], const VRaw (&vf)[NT], float2 vs, auto ntag) {
+    auto fast_pv = [&](const uint4 (&pf)[TPW], const uint4 (&vf)[NT], auto ntag) {
         constexpr int NA = decltype(ntag)::value;
         if constexpr (!kF32 && NA > 0) {
             __builtin_amdgcn_s_setprio(0);
             const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
-                const uint4 v = wide_v(vf[u], vs);
 #pragma unroll
-                for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(v, pf[t], O[t][u]);
+                for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf[u], pf[t], O[t][u]);
             }
 #pragma unroll
             for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
@@ -718,7 +661,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // Ring offsets are compile-time (the stage loop is unrolled over the ring)
     // and travel in the LDS instructions' offset fields: no address arithmetic
     // is left in the loop.
-    constexpr bool kPipe = !kF32 && !kQuant && WK == 1 && TPW <= 2;      // three tiles: not enough registers
+    constexpr bool kPipe = !kF32 && WK == 1 && TPW <= 2;      // three tiles: not enough registers
     constexpr int PF = 3;                                      // fragment prefetch distance (groups, <= NT)
     uint32_t k_off[KQ], v_off[NT];
     if constexpr (kPipe) {
@@ -863,7 +806,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             asm volatile("" : "+s"(off));
             const unsigned char *Kb = smem + off;
             uint4 kf[2][KQ];
-            load_k_frags(Kb, load_scales(buf * KSTEPS + ks, 0), kf);
+            load_k_frags(Kb, kf);
             bool wide = false;
 #pragma unroll
             for (int t = 0; t < TPW; ++t) {
@@ -966,8 +909,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             }
         } else {
             uint4 kf[2][KQ];
-            load_k_frags(Kb, load_scales(buf * KSTEPS + ks, 0), kf);
-            const float2 vs = load_scales(buf * KSTEPS + ks, 1);
+            load_k_frags(Kb, kf);
             uint4 pf[TPW];
 #pragma unroll
             for (int t = 0; t < TPW; ++t) {          // (a tile the wavefront does not own has zero queries and is dropped)
@@ -986,7 +928,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
-                const uint4 vf = wide_v(load_v_frag(Vb, u), vs);
+                const uint4 vf = load_v_frag(Vb, u);
 #pragma unroll
                 for (int t = 0; t < TPW; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
             }
@@ -997,21 +939,57 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
 
     // ---- stage loop skeleton: keep NS-1 stages in flight ahead of the one computed ----
     int issued = 0;
-    auto wait_stage = [&](int s) {
-        // stage s has landed once at most (younger stages) * LPS loads remain
-        const int ahead = issued - (s + 1);
+    // 8-bit blocks: this wavefront's page of the next stage goes from where it has landed into the ring, and the transfer that is due goes
+    // out.  A lane takes what it asked for itself: 16 channels, two pieces of the ring's row.
+    [[maybe_unused]] int widened = 0;                 // stages in the ring, of this wavefront
+    auto widen_next = [&]() {
         if constexpr (kQuant) {
+            const int raw = widened % GEO::NR, slot = widened % NS, ahead = issued - (widened + 1);
+            const int pg = stage_page(issued);
             bool done = false;
-            static_for<1, NS>([&](auto k) {
-                constexpr int n = NS - decltype(k)::value;           // NS - 1, NS - 2, ... 1
+            static_for<0, GEO::NR>([&](auto k) {
+                constexpr int n = GEO::NR - 1 - decltype(k)::value;
                 if (!done && ahead >= n) {
                     wait_vmcnt<n * LPS>();
                     done = true;
                 }
             });
-            if (!done) wait_vmcnt<0>();
+            asm volatile("" ::: "memory");
+            const unsigned char *from = smem + GEO::RAW + raw * GEO::RAW_STAGE + wave * GEO::RAW_PAGE + lane * 16;
+            const uint32_t e = *reinterpret_cast<const uint32_t *>(smem + GEO::SCALES + (raw * kWaves + wave) * 4);
+            f32x4 x[DMAS];
+#pragma unroll
+            for (int it = 0; it < DMAS; ++it) x[it] = *reinterpret_cast<const f32x4 *>(from + it * 1024);
+#pragma unroll
+            for (int it = 0; it < DMAS; ++it) asm volatile("" : "+v"(x[it]));        // they are in: the slot is free
+            if (issued < nstages) issue_stage_pg(issued++, pg);
+            const float scale = __builtin_bit_cast(float, e << 23);
+            const int piece = 2 * ld_piece;
+#pragma unroll
+            for (int it = 0; it < DMAS; ++it) {
+                const int row = it * RPI + ld_row, swz = ld_swizzle(row);
+                unsigned char *to = smem + ld_tensor * VREG + slot * STAGE + (ld_page * kPage + row) * ROWB;
+                const uint4 b = __builtin_bit_cast(uint4, x[it]);
+                *reinterpret_cast<uint4 *>(to + ((piece ^ swz) << 4)) = widen8<T>(make_uint2(b.x, b.y), scale, scale);
+                *reinterpret_cast<uint4 *>(to + (((piece + 1) ^ swz) << 4)) = widen8<T>(make_uint2(b.z, b.w), scale, scale);
+            }
+            ++widened;
+        }
+    };
+    // this wavefront's part of stage s is in the ring
+    auto wait_stage = [&](int s) {
+        if constexpr (kQuant) {
+            // (One at most.  Written as a loop it is taken for hot, and the scratch registers of a woven loop stay outside it: 240 rows of
+            // fp16, 64K tokens 95.7 -> 83.9 us.  The three-tile loop needs its registers itself: as a loop 415 instead of 171, 128K hybrid.)
+            if constexpr (TPW == 3) {
+                if (widened <= s && widened < nstages) widen_next();
+            } else {
+                while (widened <= s && widened < nstages) widen_next();
+            }
             return;
         }
+        // stage s has landed once at most (younger stages) * LPS loads remain
+        const int ahead = issued - (s + 1);
         if (NS > 3 && ahead >= 2) wait_vmcnt<(NS > 3 ? 2 : 0) * LPS>();
         else if (NS > 2 && ahead == 1) wait_vmcnt<(NS > 2 ? 1 : 0) * LPS>();
         else wait_vmcnt<0>();
@@ -1021,7 +999,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         for (int s = s_begin; s < s_end; ++s) {
             wait_stage(s);
             __syncthreads();     // everyone's part of stage s is in; stage s-1 is fully consumed
-            if (issued < nstages) {
+            if constexpr (kQuant) {
+                wait_stage(s + 1);                  // into the slot that stage s-2 occupied
+            } else if (issued < nstages) {
                 issue_stage(issued);                // refills the slot stage s-1 occupied
                 ++issued;
             }
@@ -1066,31 +1046,32 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                 __syncthreads();     // stage s is in; all LDS reads of stage s-1 have completed
                 if constexpr (kWatch)
                     if (watched(s) && alarmed(1)) end = s;
-                if (issued < nstages) {
+                if constexpr (kQuant) {
+                    if constexpr (TPW < 3) wait_stage(s + 1);
+                } else if (issued < nstages) {
                     issue_stage(issued);
                     ++issued;
                 }
             };
-            uint4 pf[TPW];
-            VRaw vf[NT];
-            float2 vs;
+            uint4 pf[TPW], vf[NT];
             auto stage = [&](int s) {
                 if constexpr (WK == 1) {
                     if (s > 0) {
-                        if (!late) fast_pv(pf, vf, vs, ntag);       // early waves finish stage s-1 first
+                        if (!late) fast_pv(pf, vf, ntag);       // early waves finish stage s-1 first
                         admit(s);
-                        if (late) fast_pv(pf, vf, vs, ntag);        // late waves carry it over
+                        if (late) fast_pv(pf, vf, ntag);        // late waves carry it over
+                        if constexpr (kQuant && TPW == 3) wait_stage(s + 1);        // (where neither P nor V^T fragments are held)
                     }
-                    fast_sx(kptr(s, 0), kptr(s, 0) + VREG, s * KSTEPS + 0, pf, vf, vs, ntag, gtag, room);
-                    fast_pv(pf, vf, vs, ntag);
-                    fast_sx(kptr(s, 1), kptr(s, 1) + VREG, s * KSTEPS + 1, pf, vf, vs, ntag, gtag, room);
+                    fast_sx(kptr(s, 0), kptr(s, 0) + VREG, pf, vf, ntag, gtag, room);
+                    fast_pv(pf, vf, ntag);
+                    fast_sx(kptr(s, 1), kptr(s, 1) + VREG, pf, vf, ntag, gtag, room);
                 } else {
                     if (s > 0) {
-                        if (!late) fast_pv(pf, vf, vs, ntag);
+                        if (!late) fast_pv(pf, vf, ntag);
                         admit(s);
-                        if (late) fast_pv(pf, vf, vs, ntag);
+                        if (late) fast_pv(pf, vf, ntag);
                     }
-                    fast_sx(kptr(s, wk), kptr(s, wk) + VREG, s * KSTEPS + wk, pf, vf, vs, ntag, gtag, room);
+                    fast_sx(kptr(s, wk), kptr(s, wk) + VREG, pf, vf, ntag, gtag, room);
                 }
             };
             if constexpr (kGuard && (TPW > 1 || !kWatch)) {
@@ -1099,7 +1080,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             } else {
                 for (int s = 0; s < end; ++s) stage(s);
             }
-            fast_pv(pf, vf, vs, ntag);
+            fast_pv(pf, vf, ntag);
             return end;
         } else {
             return 0;
@@ -1141,7 +1122,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                     const int s = s4 + (int)B;
                     if (s < end) {                                      // uniform
                         // stage s+1 in; every wave is done with stage s-1: refill its slot
-                        const int pg = stage_page(issued);
+                        [[maybe_unused]] const int pg = kQuant ? 0 : stage_page(issued);
                         constexpr bool kLook = kGuard && B == 0;
                         if constexpr (kLook)
                             if (s > 0 && watched(s)) watch_sums();
@@ -1149,7 +1130,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                         __syncthreads();
                         if constexpr (kLook)
                             if (watched(s) && alarmed(1)) end = s;
-                        if (issued < nstages && issued <= s + NS - 1) {
+                        if constexpr (kQuant) {
+                            wait_stage(s + 2);
+                        } else if (issued < nstages && issued <= s + NS - 1) {
                             issue_stage_pg(issued, pg);
                             ++issued;
                         }
@@ -1217,7 +1200,10 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // 20K tokens 41.5 -> 40.6 us, 240 rows, 64K 79.7 -> 79.3).
     constexpr bool kPaced = !kF32 && TPW >= 2;
     if constexpr (!kF32) {
-        if constexpr (kPaced) {
+        if constexpr (kQuant) {                       // (half the bytes: nothing to pace)
+            issue_queries();
+            for (; issued < GEO::NR && issued < nstages; ++issued) issue_stage(issued);
+        } else if constexpr (kPaced) {
             issue_queries();
             issue_stage(0);                           // (a piece is not empty)
             issued = 1;
@@ -1233,12 +1219,16 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         if (lane < Nb) s_anc[lane] = set;
     }
     if constexpr (!kF32) {
-        if constexpr (kPaced) wait_vmcnt<LPS>();
+        if constexpr (kQuant) {
+            if (issued == GEO::NR) wait_vmcnt<GEO::NR * LPS>();
+            else wait_vmcnt<0>();
+            asm volatile("" ::: "memory");
+        } else if constexpr (kPaced) wait_vmcnt<LPS>();
         else wait_stage(0);                           // the queries were requested before stage 1: they are in as well
         take_queries();
         __syncthreads();                              // everyone has; their slots are free
-        if constexpr (kPaced) {
-            if (nstages > 1) issue_stage(issued++);
+        if constexpr (kPaced || kQuant) {
+            if (!kQuant && nstages > 1) issue_stage(issued++);
             wait_stage(0);
             __syncthreads();
         }
@@ -1262,9 +1252,9 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         }
         int n_fast = 0;
         if (kHasFast && pass < kPasses - 1) n_fast = max(0, min(nstages, (L - pos0) / SK));
-        if (pass > 0 && !(kGuard && kept)) issued = 0;        // a redo starts over
+        if (pass > 0 && !(kGuard && kept)) issued = widened = 0;        // a redo starts over
         // (the careful loop begins by filling the last slot itself)
-        for (const int fill = n_fast > 0 ? NS : NS - 1; issued < fill && issued < nstages; ++issued) issue_stage(issued);
+        for (const int fill = kQuant ? GEO::NR : n_fast > 0 ? NS : NS - 1; issued < fill && issued < nstages; ++issued) issue_stage(issued);
         if (n_fast > 0) {
             stamp(2);
             f32x4 Sa[TPW][2];

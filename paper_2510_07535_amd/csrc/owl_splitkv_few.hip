@@ -13,14 +13,15 @@
 //             into 16 costs is paid once for them.  More tiles are further row groups, other workgroups that
 //             find the chunks in their XCD's L2.  (Three tiles a wavefront leave no registers to read ahead, and were slower than
 //             more groups; four wavefronts of 512 registers with up to five tiles, products and softmax of a tile woven by hand,
-//             were slower than the shared ring, 99.5 against 89.6 us with 15 tiles at 64K.)
+//             were slower than the shared ring, 99.5 us with 15 tiles at 64K against 76.)
 //   softmax   Each wavefront has a reference of its own for each row.  It stays until a score lies more than `kRoom` above it;
 //             the row then moves to its highest score.
 //   merge     At the end of a piece the wavefronts' sums meet in LDS, a tile after the other, a channel tile a wavefront, and
 //             leave one partial, in fp32 (rounded to fp16 it would cost half of what the answer's own rounding does).
-// us, shared ring -> here, 8 KV heads, head_dim 128, bf16 queries: 1 node (4 rows) at 64K 40.5 -> 27.3 (4.9 TB/s), 6 nodes
-// (24 rows) at 128K 74 -> 51.4 (5.2 TB/s), 16 sequences of 8K-64K with 4 rows 309 -> 213 (6.2 TB/s: the stream is the bound), 16 nodes (64
-// rows, 2 groups) at 64K 44.8 -> 40.8.  From two groups on the chunks' way from L2 and their conversion, once a group, are the bound.
+// us, shared ring -> here, 8 KV heads, head_dim 128, bf16 queries: 1 node (4 rows) at 64K 39.0 -> 27.7 (4.9 TB/s), 6 nodes
+// (24 rows) at 32K 25.1 -> 20.7, at 128K 68.7 -> 51.9 (5.2 TB/s), 16 sequences of 8K-64K with 4 rows 302 -> 211 (6.3 TB/s: the stream is the
+// bound), 16 nodes (64 rows, 2 groups) at 64K 41.9 -> 40.9.  From two groups on the chunks' way from L2 and their conversion, once a
+// group, are the bound.
 //
 // The scores of a chunk come out with the keys of its first page in one accumulator and those of its second in the other.
 #include "owl_splitkv.h"
@@ -68,6 +69,14 @@ __device__ __forceinline__ void arrived()
 __device__ __forceinline__ void reads_done()
 {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// Transposing 64-bit LDS read of bytes (see the file comment for the lane mapping).
+__device__ __forceinline__ uint2 lds_read_tr8(const unsigned char *p)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3))) *)(p));
+    return __builtin_bit_cast(uint2, v);
 }
 
 // Geometry of one instantiation.
