@@ -391,7 +391,8 @@ owl_status owl_append_kv(const owl_verify_desc *desc, const owl_append_desc *app
  * owl_append_kv_quant: owl_append_kv into such a cache.  The rows that
  * owl_append_kv would store are what is rounded to 8 bits.  In the block that
  * holds position ctx_lens[b] the rows before it count for the scale and are kept, rows
- * behind the last new one are not touched and do not count.
+ * behind the last new one are not touched and do not count.  A sequence without new rows
+ * keeps its blocks as they are.
  */
 owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_desc *append, const void *q,
                                const void *k_new, const void *v_new, const float *inv_freq, const int32_t *pos_ids,

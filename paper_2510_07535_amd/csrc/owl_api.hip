@@ -311,11 +311,11 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
 owl_status ensure_lds_attr(const Variant *v)
 {
     static std::mutex mu;
-    static bool done[16][80] = {};
+    static bool done[16][64] = {};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return OWL_ERR_HIP;
     const int vi = variant_index(v);
-    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 80) return OWL_ERR_HIP;
+    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 64) return OWL_ERR_HIP;
     std::lock_guard<std::mutex> lock(mu);
     if (!done[dev][vi]) {
         if (hipFuncSetAttribute(v->func, hipFuncAttributeMaxDynamicSharedMemorySize,

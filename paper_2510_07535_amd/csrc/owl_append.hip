@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     bool good;
     const int L = append_len(p, b, teller, &good), block = L / kPage + (int)blockIdx.x;
     const int first = block * kPage - L;                     // new token of slot 0; negative: rows before the context's end
-    if (first >= n_b) return;
+    if (first >= n_b || n_b == 0) return;                    // (no new row: the block stays as it is)
     const int page = good ? append_page(p, b, block, teller) : -1;
     const int half = p.rot_dim / 2, turned = p.rot_dim / (2 * E);
     if (tid < 2) s_big[tid] = 0;

@@ -75,7 +75,7 @@ struct VariantList {
     int count;
 };
 VariantList quant_variants();      // owl_splitkv_quant.hip
-VariantList few_tile_variants();   // owl_splitkv_few.hip: caches of 8-bit blocks too, wr = 1, wk = 8
+VariantList few_tile_variants();   // owl_splitkv_few.hip: caches of 8-bit blocks too; wk = 8, wr = 1 or, one of several row groups, 2
 int variant_index(const Variant *v);
 
 // Profiling hook state (set through the probe interface; read by the verify entry points).

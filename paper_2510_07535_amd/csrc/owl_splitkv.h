@@ -411,6 +411,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
     // applied to the global address, the LDS side of the transfer is always
     // lane-linear.  Slots past the end of the split (ragged last stage only)
     // re-read the last valid row: finite data whose scores are masked out later.
+    // (8-bit blocks travel as they lie, into the wavefront's own slots; widen_next permutes.)
     const int ld_tensor = wave >> 2, ld_page = wave & 3;
     const unsigned char *ld_base = static_cast<const unsigned char *>(ld_tensor ? p.v : p.k);
     const int last_pgx = (pos1 - 1 - pos0) >> 4, last_slot = (pos1 - 1) & (kPage - 1);

@@ -223,7 +223,7 @@ __device__ __forceinline__ void run_quant_piece(const QuantParams &p, unsigned c
     for (int t = 0; t < TPW; ++t) {
         const int tg = rg * p.group_tiles + t;
         const bool tile_ok = t < p.group_tiles && tg < p.RT;
-        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.hip)
+        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
         const unsigned char *src = q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2);

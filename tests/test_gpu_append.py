@@ -137,6 +137,22 @@ def test_sequences_with_fewer_new_tokens_and_without_queries(dtype, quant):
     assert (a.q_out == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+def test_a_sequence_without_new_tokens_keeps_its_block(dtype):
+    """Its rows could do with a smaller scale; the other sequence's block, of the same kind, gets one."""
+    a = Append(14, dtype=dtype, quant=True, Hq=4, Hkv=2, D=64, ctx=[5, 5, 0], n=3, rot_dim=64, counts=np.array([0, 3, 0], np.int32), spread=0)
+    for blocks, raw, scale in ((a.k, a.dev[0], a.dev[2]), (a.v, a.dev[1], a.dev[3])):
+        blocks.flat &= 0xBF                              # magnitudes below 2
+        blocks.scale += 4
+        raw &= 0xBF
+        scale += 4
+    before = [t.clone() for t in a.dev]
+    a.run()
+    a.check()
+    for got, was in zip(a.dev[2:], before[2:]):
+        assert torch.equal(got[a.table[0, 0]], was[a.table[0, 0]]) and (got[a.table[1, 0]] < was[a.table[1, 0]]).all()
+
+
 @pytest.mark.parametrize("dtype,quant", [(W.DT_BF16, False), (W.DT_F32, False), (W.DT_F16, True)])
 def test_queries_in_place(dtype, quant):
     a = Append(6, dtype=dtype, quant=quant, Hq=8, Hkv=2, D=128, ctx=[11], n=21, rot_dim=96, fused=False)
