@@ -101,14 +101,17 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // outgrowing the K/V they summarise: then the rows are cut into more, smaller
     // groups instead, each re-reading the split from its XCD's L2.
     int tpw, wr, wk, rgs, group_tiles;
-    // Over 8-bit blocks few tiles go to wavefronts with keys of their own, two tiles a row group (owl_splitkv_few.hip), many to
-    // the shared ring.  us, ring -> own keys, 8 KV heads, head_dim 128, bf16: 64K context, 1 tile 39.0 -> 27.7, 3 40.9 -> 39.5, 4 41.9 -> 40.9, 5
-    // 51.3 -> 51.1, 6 51.6 -> 51.5, 7 52.7 -> 59.6, 8 55.1 -> 60.7; 16 sequences of 8K-64K, 1 tile 302 -> 211, 3 312 -> 296, 4 331 -> 298, 5 389 ->
-    // 425, 6 410 -> 426, 7 408 -> 507 (more groups read each key from L2 and widen it again).  Short streams gain longer: 8 tiles of 1 KV
-    // head 20.8 -> 17.6, of 2 24.5 -> 23.1, of 4 34.1 -> 35.0.  So does fp16, whose ring guards its references: 5 tiles 59.1 -> 51.4, 7 63.3 ->
-    // 59.1, in the batch 5 480 -> 421, 6 485 -> 430, 7 438 -> 500.
-    const bool lone = d->batch == 1;
-    const bool few = quant && RT <= (d->qkv_dtype == OWL_F16 ? (lone ? 8 : 6) : !lone ? 4 : d->n_kv_heads > 2 ? 6 : 8);
+    // Over 8-bit blocks little work goes to wavefronts with keys of their own, two tiles a row group (owl_splitkv_few.hip), much to
+    // the shared ring.  A lone sequence of up to four tiles, and of more as long as what the row groups read again, tokens x tiles x KV heads, is
+    // less than what the ring's barriers cost.  Own keys / ring, head_dim 128, by that product: bf16, 0.2-0.6 M 0.84-0.97, 0.6-0.9 M 0.86-0.96,
+    // 1.0-1.1 M 0.87-1.05, 1.2-1.3 M 0.93-1.05, 2-3 M 0.79-1.12, 4.7 M 1.16, 7.9 M 1.36; fp16, whose ring guards its references, below 4 M 0.71-0.94,
+    // 4.7 M 0.99, 4.8 M 1.06, 7.9 M 1.16; up to four tiles of 64K tokens (8 heads) 0.71, 0.76, 0.97, 0.98.  In a batch nothing is left over for
+    // groups that read again: 16 sequences of 200-600, 500-2K, 2K-8K, 8K-64K, 64 of 500-2K and 4 of 4K-20K, bf16, 1 tile 0.77 0.67 0.68 0.70 0.61 0.72, 2
+    // 0.87 0.86 0.73 - 0.79 0.89, 4 1.06 1.02 1.01 0.90 1.11 0.95, 5 1.22 1.16 1.10 1.09 1.25 1.00; fp16, 4 1.00 0.91 0.87 0.81 1.00 0.85, 5 1.11 0.96
+    // 0.90 0.88 1.11 0.85, 6 1.10 0.96 0.96 0.89 1.14 0.84, 7 (8K-64K) 1.14.
+    const bool fp16 = d->qkv_dtype == OWL_F16;
+    const bool few = quant && (d->batch == 1 ? RT <= 4 || T * RT * d->n_kv_heads <= (fp16 ? 4000000 : 1100000)
+                                             : RT <= (fp16 ? (d->max_ctx_len < 4096 ? 4 : 6) : (d->max_ctx_len < 16384 ? 2 : 4)));
     if (few) {
         rgs = (RT + 1) / 2;
         group_tiles = (RT + rgs - 1) / rgs;

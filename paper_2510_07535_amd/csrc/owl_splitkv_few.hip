@@ -1,5 +1,5 @@
-// Split-KV pass of the verify-step attention over a cache of 8-bit blocks for few query rows, one to eight 16-row tiles of a KV
-// head, for gfx950 (MI355X).
+// Split-KV pass of the verify-step attention over a cache of 8-bit blocks for few query rows, or short contexts, for gfx950
+// (MI355X); which calls come here is the plan's to say.
 //
 // The share of a workgroup, its pieces, their partials, and how 8 bits become operands of 16 are those of owl_splitkv.h; the loop
 // is another one.  Half the bytes arrive in half the time, so what bounds the shared ring beside its stream, eight wavefronts that
@@ -20,7 +20,7 @@
 //             leave one partial, in fp32 (rounded to fp16 it would cost half of what the answer's own rounding does).
 // us, shared ring -> here, 8 KV heads, head_dim 128, bf16 queries: 1 node (4 rows) at 64K 39.0 -> 27.7 (4.9 TB/s), 6 nodes
 // (24 rows) at 32K 25.1 -> 20.7, at 128K 68.7 -> 51.9 (5.2 TB/s), 16 sequences of 8K-64K with 4 rows 302 -> 211 (6.3 TB/s: the stream is the
-// bound), 16 nodes (64 rows, 2 groups) at 64K 41.9 -> 40.9.  From two groups on the chunks' way from L2 and their conversion, once a
+// bound), 16 nodes (64 rows, 2 groups) at 64K 41.9 -> 40.9, 60 nodes (240 rows, 8 groups) on 5K in fp16 22.7 -> 19.0.  From two groups on the chunks' way from L2 and their conversion, once a
 // group, are the bound.
 //
 // The scores of a chunk come out with the keys of its first page in one accumulator and those of its second in the other.

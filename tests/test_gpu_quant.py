@@ -112,6 +112,52 @@ def test_every_number_of_row_tiles(n, ctx, D):
     assert step.flags() == 0
 
 
+def _announced(bc, most):
+    """A step whose sequences may be ``most`` long: its work is dealt out as that of long ones."""
+    step = QuantStep(bc)
+    wide = (most + bc.case.N + 15) // 16
+    table = np.full((bc.case.B, wide), -1, np.int32)
+    table[:, :bc.case.page_table.shape[1]] = bc.case.page_table
+    step.table = i32(table)
+    step.desc.max_ctx_len, step.desc.max_pages_per_seq = most, wide
+    step.workspace = torch.empty(B.owl_verify_attn_quant_workspace_size(step.desc), dtype=torch.uint8, device=DEV)
+    return step
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,group", [(20, 4), (28, 4), (32, 4), (40, 4), (60, 4), (40, 8), (64, 8), (50, 16)])
+def test_sequences_announced_as_long_ones(n, group, D, dtype):
+    """Every layout of the loop that many rows share, on lengths of a few stages to some seventy."""
+    r = rng(n + group + D)
+    for hkv, ctx in ((2, [4500]), (1, [700]), (2, [1, 1030, 64])):
+        bc = block_case("quant-announced", n, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=D, ctx_lens=ctx, trees=_trees("tree", n, len(ctx), r))
+        step = _announced(bc, 1 << 20)
+        step.run()
+        assert_attention(step.result(), bc, oracle_out(bc), f"{hkv} {ctx}")
+        assert step.flags() == 0
+
+
+@pytest.mark.parametrize("dtype,gain", [(W.DT_BF16, 32.0), (W.DT_BF16, 64.0), (W.DT_F16, 4.0), (W.DT_F16, 16.0)])
+@pytest.mark.parametrize("n,group", [(28, 4), (32, 4), (60, 4), (40, 8)])
+def test_outgrown_references_of_sequences_announced_as_long_ones(n, group, dtype, gain):
+    r = rng(n + int(gain))
+    bc = block_case("quant-outgrown", 3, dtype=dtype, Hq=2 * group, Hkv=2, D=128, ctx_lens=[3001], trees=_trees("tree", n, 1, r), outlier_frac=0.05,
+                    outlier_gain=gain)
+    step = _announced(bc, 1 << 20)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+def test_more_row_groups_than_an_xcd_has_compute_units(dtype):
+    r = rng(9)
+    bc = block_case("quant-rows", 9, dtype=dtype, Hq=32, Hkv=1, D=128, ctx_lens=[500], trees=_trees("tree", 64, 1, r))
+    step = QuantStep(bc)
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
 def test_answers_in_16_bits_and_zeros_of_absent_nodes():
     r = rng(1)
     for dtype, kind in ((W.DT_BF16, B.OWL_BF16), (W.DT_F16, B.OWL_F16)):
