@@ -138,6 +138,21 @@ def test_sequences_with_fewer_new_tokens_and_without_queries(dtype, quant):
 
 
 @pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("Hkv,D,pairs", [(2, 128, False), (3, 64, True)])
+def test_blocks_with_gaps_between_their_rows(dtype, Hkv, D, pairs):
+    """Bytes between rows, heads and pages, that stay as they are."""
+    a = Append(15, dtype=dtype, quant=True, Hq=2 * Hkv, Hkv=Hkv, D=D, ctx=[21, 40, 0], n=19, rot_dim=D // 2, pairs=pairs)
+    head, token = D + 16, Hkv * (D + 16) + 32
+    page = 16 * token + 48
+    a.strides, r = (page, head, token), rng(16)
+    a.desc.kv_stride_page, a.desc.kv_stride_head, a.desc.kv_stride_token = a.strides
+    a.k, a.v = (C.Blocks(r.integers(0, 256, a.n_pages * page).astype(np.uint8) & 0xF7, x.scale, a.strides, D, dtype) for x in (a.k, a.v))
+    a.dev = [torch.from_numpy(t).to(DEV) for t in (a.k.flat, a.v.flat, a.k.scale, a.v.scale)]
+    a.run()
+    a.check()
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
 def test_a_sequence_without_new_tokens_keeps_its_block(dtype):
     """Its rows could do with a smaller scale; the other sequence's block, of the same kind, gets one."""
     a = Append(14, dtype=dtype, quant=True, Hq=4, Hkv=2, D=64, ctx=[5, 5, 0], n=3, rot_dim=64, counts=np.array([0, 3, 0], np.int32), spread=0)

@@ -158,6 +158,59 @@ def test_more_row_groups_than_an_xcd_has_compute_units(dtype):
     assert_attention(step.result(), bc, oracle_out(bc))
 
 
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,long", [(6, False), (40, False), (60, True)])
+def test_gaps_between_rows_heads_and_pages(n, long, D, dtype):
+    r = rng(n + D)
+    bc = block_case("quant-gaps", 4, dtype=dtype, Hq=8, Hkv=2, D=D, ctx_lens=[1203], trees=_trees("tree", n, 1, r))
+    step = _announced(bc, 1 << 20) if long else QuantStep(bc)
+    token = 2 * (D + 16) + 32
+    strides = (16 * token + 48, D + 16, token)
+    for name, blocks in (("k", bc.k), ("v", bc.v)):
+        wide = C.Blocks(np.full(bc.case.n_pool_pages * strides[0], NAN_BYTE, np.uint8), blocks.scale, strides, D, dtype)
+        for page in range(bc.case.n_pool_pages):
+            for g in range(2):
+                for slot in range(16):
+                    wide.flat[wide._at(page, g, slot)] = blocks.flat[blocks._at(page, g, slot)]
+        setattr(step, name, torch.from_numpy(wide.flat).to(DEV))
+    step.desc.kv_stride_page, step.desc.kv_stride_head, step.desc.kv_stride_token = strides
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+
+
+def test_captured_calls_on_two_streams_at_once():
+    """A short and an announced-as-long sequence, each in a graph on its own stream with its own workspace, replayed side by side."""
+    r = rng(12)
+    steps, graphs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for long, n, dtype in ((False, 12, W.DT_F16), (True, 40, W.DT_BF16)):
+        bc = block_case("quant-two", n, dtype=dtype, Hq=16, Hkv=2, D=128, ctx_lens=[2100], trees=_trees("tree", n, 1, r))
+        step = _announced(bc, 1 << 20) if long else QuantStep(bc)
+        B.owl_verify_attn_quant_init(step.desc)
+        step.run()
+        steps.append((step, step.result(), bc))
+    for (step, _, _), stream in zip(steps, streams):
+        graph = torch.cuda.CUDAGraph()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+            for _ in range(3):
+                step.run()
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for rep in range(4):
+        for step, _, _ in steps:
+            step.out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        for step, want, bc in steps:
+            got = step.result()
+            assert np.array_equal(got, want), rep
+    for step, want, bc in steps:
+        assert_attention(want, bc, oracle_out(bc))
+
+
 def test_answers_in_16_bits_and_zeros_of_absent_nodes():
     r = rng(1)
     for dtype, kind in ((W.DT_BF16, B.OWL_BF16), (W.DT_F16, B.OWL_F16)):
