@@ -211,6 +211,35 @@ def test_captured_calls_on_two_streams_at_once():
         assert_attention(want, bc, oracle_out(bc))
 
 
+@pytest.mark.parametrize("n,long", [(6, False), (60, True)])
+def test_pages_beyond_32_bit_offsets(n, long):
+    """The attention and the commit where pages lie 4 GB behind the first one."""
+    r = rng(n)
+    bc = block_case("quant-far", 4, dtype=W.DT_BF16, Hq=32, Hkv=8, D=128, ctx_lens=[700], trees=_trees("tree", n, 1, r))
+    step = _announced(bc, 1 << 20) if long else QuantStep(bc)
+    page, count = 8 * 16 * 128, bc.case.n_pool_pages
+    pages = (1 << 32) // page + 2 * count
+    far = pages - count
+    for name in ("k", "v", "ks", "vs"):
+        near = getattr(step, name)
+        wide = torch.empty(pages * (near.numel() // count), dtype=torch.uint8, device=DEV)
+        wide[far * (near.numel() // count):] = near.reshape(-1)
+        setattr(step, name, wide)
+    step.table = torch.where(step.table >= 0, step.table + far, step.table)
+    step.desc.n_pool_pages = pages
+    step.run()
+    assert_attention(step.result(), bc, oracle_out(bc))
+    acc = np.full((1, n), -1, np.int32)
+    acc[0, :3] = 1, 2, 5
+    B.owl_commit_kv_quant(step.desc, step.k, step.v, step.ks, step.vs, step.table, step.lens, i32(acc), i32([3]), None, step.status)
+    for blocks, raw, scale in ((bc.k, step.k, step.ks), (bc.v, step.v, step.vs)):
+        want = blocks.copy()
+        want.commit(bc.case.page_table, bc.case.ctx_lens, acc, [3])
+        assert np.array_equal(scale[far * 8:].cpu().numpy().reshape(want.scale.shape), want.scale)
+        assert C.same_bytes(raw[far * page:].cpu().numpy(), want.flat)
+    assert step.flags() == 0
+
+
 def test_answers_in_16_bits_and_zeros_of_absent_nodes():
     r = rng(1)
     for dtype, kind in ((W.DT_BF16, B.OWL_BF16), (W.DT_F16, B.OWL_F16)):
