@@ -940,13 +940,14 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
 
     // ---- stage loop skeleton: keep NS-1 stages in flight ahead of the one computed ----
     int issued = 0;
-    // 8-bit blocks: this wavefront's page of the next stage goes from where it has landed into the ring, and the transfer that is due goes
-    // out.  A lane takes what it asked for itself: 16 channels, two pieces of the ring's row.
+    // 8-bit blocks: this wavefront's page of the next stage goes from where it has landed (widen_take) into the ring (widen_put), and the
+    // transfer that is due goes out.  A lane takes what it asked for itself: 16 channels, two pieces of the ring's row.
     [[maybe_unused]] int widened = 0;                 // stages in the ring, of this wavefront
-    auto widen_next = [&]() {
+    f32x4 raw_page[kQuant ? DMAS : 1];
+    uint32_t raw_scale = 0;
+    auto widen_take = [&]() {
         if constexpr (kQuant) {
-            const int raw = widened % GEO::NR, slot = widened % NS, ahead = issued - (widened + 1);
-            const int pg = stage_page(issued);
+            const int raw = widened % GEO::NR, ahead = issued - (widened + 1);
             bool done = false;
             static_for<0, GEO::NR>([&](auto k) {
                 constexpr int n = GEO::NR - 1 - decltype(k)::value;
@@ -957,25 +958,33 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
             });
             asm volatile("" ::: "memory");
             const unsigned char *from = smem + GEO::RAW + raw * GEO::RAW_STAGE + wave * GEO::RAW_PAGE + lane * 16;
-            const uint32_t e = *reinterpret_cast<const uint32_t *>(smem + GEO::SCALES + (raw * kWaves + wave) * 4);
-            f32x4 x[DMAS];
+            raw_scale = *reinterpret_cast<const uint32_t *>(smem + GEO::SCALES + (raw * kWaves + wave) * 4);
 #pragma unroll
-            for (int it = 0; it < DMAS; ++it) x[it] = *reinterpret_cast<const f32x4 *>(from + it * 1024);
+            for (int it = 0; it < DMAS; ++it) raw_page[it] = *reinterpret_cast<const f32x4 *>(from + it * 1024);
+        }
+    };
+    auto widen_put = [&]() {
+        if constexpr (kQuant) {
+            const int slot = widened % NS, pg = stage_page(issued);
 #pragma unroll
-            for (int it = 0; it < DMAS; ++it) asm volatile("" : "+v"(x[it]));        // they are in: the slot is free
+            for (int it = 0; it < DMAS; ++it) asm volatile("" : "+v"(raw_page[it]));        // they are in: the slot is free
             if (issued < nstages) issue_stage_pg(issued++, pg);
-            const float scale = __builtin_bit_cast(float, e << 23);
+            const float scale = __builtin_bit_cast(float, raw_scale << 23);
             const int piece = 2 * ld_piece;
 #pragma unroll
             for (int it = 0; it < DMAS; ++it) {
                 const int row = it * RPI + ld_row, swz = ld_swizzle(row);
                 unsigned char *to = smem + ld_tensor * VREG + slot * STAGE + (ld_page * kPage + row) * ROWB;
-                const uint4 b = __builtin_bit_cast(uint4, x[it]);
+                const uint4 b = __builtin_bit_cast(uint4, raw_page[it]);
                 *reinterpret_cast<uint4 *>(to + ((piece ^ swz) << 4)) = widen8<T>(make_uint2(b.x, b.y), scale, scale);
                 *reinterpret_cast<uint4 *>(to + (((piece + 1) ^ swz) << 4)) = widen8<T>(make_uint2(b.z, b.w), scale, scale);
             }
             ++widened;
         }
+    };
+    auto widen_next = [&]() {
+        widen_take();
+        widen_put();
     };
     // this wavefront's part of stage s is in the ring
     auto wait_stage = [&](int s) {
@@ -1048,7 +1057,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                 if constexpr (kWatch)
                     if (watched(s) && alarmed(1)) end = s;
                 if constexpr (kQuant) {
-                    if constexpr (TPW < 3) wait_stage(s + 1);
+                    if constexpr (TPW < 3 && WK == 1) wait_stage(s + 1);
                 } else if (issued < nstages) {
                     issue_stage(issued);
                     ++issued;
@@ -1072,7 +1081,12 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                         admit(s);
                         if (late) fast_pv(pf, vf, ntag);
                     }
+                    // (8-bit blocks: the next page's reads and its stores, with the scores and their exponentials between them: 104 rows, 16
+                    // sequences of 8K-64K 417 -> 406 us, fp16 437 -> 420)
+                    const bool next = kQuant && widened <= s + 1 && widened < nstages;
+                    if (next) widen_take();
                     fast_sx(kptr(s, wk), kptr(s, wk) + VREG, pf, vf, ntag, gtag, room);
+                    if (next) widen_put();
                 }
             };
             if constexpr (kGuard && (TPW > 1 || !kWatch)) {
@@ -1131,8 +1145,15 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                         __syncthreads();
                         if constexpr (kLook)
                             if (watched(s) && alarmed(1)) end = s;
+                        // (8-bit blocks: with one tile the next page's reads and stores go before and behind the first step, 80 rows, 16
+                        // sequences of 8K-64K 389 -> 377 us; with two there are no registers for it in between)
+                        const bool next = kQuant && TPW == 1 && widened <= s + 2 && widened < nstages;
                         if constexpr (kQuant) {
-                            wait_stage(s + 2);
+                            if constexpr (TPW == 1) {
+                                if (next) widen_take();
+                            } else {
+                                wait_stage(s + 2);
+                            }
                         } else if (issued < nstages && issued <= s + NS - 1) {
                             issue_stage_pg(issued, pg);
                             ++issued;
@@ -1141,6 +1162,7 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                         pipe_iter(Sb, Sa, Pa, Pb, vpre, std::integral_constant<uint32_t, cur0>{},
                                   std::integral_constant<uint32_t, nxt0>{}, std::integral_constant<uint32_t, cur1>{},
                                   yes{}, ntag);
+                        if (next) widen_put();
                         // step 2s+2: its P; O += V^T P of step 2s+1; scores of step 2s+3.  After the
                         // last fast stage only the V^T P part counts: the P and the scores it
                         // produces belong to steps the careful loop redoes, and are dropped.
