@@ -103,12 +103,12 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     int tpw, wr, wk, rgs, group_tiles;
     // Over 8-bit blocks little work goes to wavefronts with keys of their own, two tiles a row group (owl_splitkv_few.hip), much to
     // the shared ring.  A lone sequence of up to four tiles, and of more as long as what the row groups read again, tokens x tiles x KV heads, is
-    // less than what the ring's barriers cost.  Own keys / ring, head_dim 128, by that product: bf16, 0.2-0.6 M 0.84-0.97, 0.6-0.9 M 0.86-0.96,
-    // 1.0-1.1 M 0.87-1.05, 1.2-1.3 M 0.93-1.05, 2-3 M 0.79-1.12, 4.7 M 1.16, 7.9 M 1.36; fp16, whose ring guards its references, below 4 M 0.71-0.94,
-    // 4.7 M 0.99, 4.8 M 1.06, 7.9 M 1.16; up to four tiles of 64K tokens (8 heads) 0.71, 0.76, 0.97, 0.98.  In a batch nothing is left over for
-    // groups that read again: 16 sequences of 200-600, 500-2K, 2K-8K, 8K-64K, 64 of 500-2K and 4 of 4K-20K, bf16, 1 tile 0.77 0.67 0.68 0.70 0.61 0.72, 2
-    // 0.87 0.86 0.73 - 0.79 0.89, 4 1.06 1.02 1.01 0.90 1.11 0.95, 5 1.22 1.16 1.10 1.09 1.25 1.00; fp16, 4 1.00 0.91 0.87 0.81 1.00 0.85, 5 1.11 0.96
-    // 0.90 0.88 1.11 0.85, 6 1.10 0.96 0.96 0.89 1.14 0.84, 7 (8K-64K) 1.14.
+    // less than what the ring's barriers cost.  Own keys / ring, head_dim 128, more than four tiles, by that
+    // product: bf16, below 0.9 M 0.82-1.01, 0.9-1.1 M 0.88 and 1.04, 1.1-1.4 M 0.94-1.07, 1.4-2.1 M 0.81-1.08, 2.1-4 M 1.05-1.15, above 1.2-1.4; fp16, whose
+    // ring guards its references, below 4 M 0.73-0.99, 4-5 M 0.99 and 1.06, 7.9 M 1.14; 1, 2, 3 and 4 tiles of 64K tokens, 8 heads, 0.74 0.78 0.96
+    // 0.96.  In a batch nothing is left over for groups that read again: 16 sequences of 200-600, 500-2K, 2K-8K, 8K-64K, 64 of 500-2K and 4 of
+    // 4K-20K, bf16, 1 tile 0.74 0.67 0.69 0.72 0.63 0.73, 2 0.86 0.85 0.74 0.74 0.79 0.87, 4 1.07 1.01 0.96 0.92 1.10 0.93, 5 1.23 1.16 1.10 1.13 1.31 1.03;
+    // fp16, 4 1.01 0.93 0.92 0.89 1.03 0.88, 5 1.13 0.99 0.94 0.92 1.15 0.86, 6 1.12 0.98 0.99 0.93 1.18 0.90, 7 (8K-64K) 1.20.
     const bool fp16 = d->qkv_dtype == OWL_F16;
     const bool few = quant && (d->batch == 1 ? RT <= 4 || T * RT * d->n_kv_heads <= (fp16 ? 4000000 : 1100000)
                                              : RT <= (fp16 ? (d->max_ctx_len < 4096 ? 4 : 6) : (d->max_ctx_len < 16384 ? 2 : 4)));
