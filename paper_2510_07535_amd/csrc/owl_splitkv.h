@@ -1331,6 +1331,23 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         }
     }
 
+    // ---- 8-bit blocks, bf16: a row's sums leave with a reference at their own size ----
+    // A merge drops what lies 2^126 below its highest reference.  Lifted, a reference may lie 40 above a row's greatest score, that of
+    // another piece or key group 100 below its own: the greater of two sums could be dropped.  Here the row sum's power of two goes
+    // into the reference, which leaves the sum in [1, 2).  (Exact but for the reference's own rounding, 2^-16 up to 256.)
+    if constexpr (kLift > 0.0f) {
+#pragma unroll
+        for (int t = 0; t < TPW; ++t) {
+            const float l = O[t][NT][0];
+            if (!(l > 0.f && l < 1.0e30f)) continue;                      // no key seen, or no number
+            const int e = (int)(__builtin_bit_cast(uint32_t, l) >> 23) - 127;
+            const float back = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+            m[t] += (float)e;
+#pragma unroll
+            for (int u = 0; u <= NT; ++u) O[t][u] *= back;
+        }
+    }
+
     // ---- merge the two key groups of a row group through LDS (reuses the ring), 16 bytes a lane ----
     // With one tile a wavefront the second group hands its tile to the first.  With two, each hands one over and finishes
     // the other, so that all eight wavefronts write partials.
