@@ -1316,7 +1316,20 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
         if (!kHasFast || pass == kPasses - 1) break;
         bool bad = false;
 #pragma unroll
-        for (int t = 0; t < TPW; ++t) bad |= !(O[t][NT][0] < 1.0e30f);
+        for (int t = 0; t < TPW; ++t) {
+            const float l = O[t][NT][0];
+            bad |= !(l < 1.0e30f);
+            // Lifted weights of 2^-40 take values below 2^-60 or so out of what 32 bits hold, and weights that grew to 2^99 those above
+            // 2^28.  The exact loop, whose greatest weight is 1, serves both.  (Each lane asks its own channels, a quarter of the row's.)
+            if constexpr (kLift > 0.0f) {
+                float big = 0.f;
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) big = fmaxf(big, fabsf(O[t][u][r]));
+                bad |= l > 0.f && !(big > 0x1p-90f && big < 0x1p100f);
+            }
+        }
         if (!workgroup_any(bad, wave, lane, s_any + kWaves)) break;
         if constexpr (kGuard) {
             __syncthreads();

@@ -114,9 +114,19 @@ def test_the_greatest_score_among_keys_that_began_far_below(layout, odd, D, dtyp
 
 
 # --------------------------------------------------------------------------- towards the ends of the types
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_great_values_where_scores_outgrow_the_first_ones(layout, D):
+    """A weight of up to 2^99 beside its piece's reference, times values of 2^60."""
+    split = LAYOUTS[layout][-1]
+    step, bc = scored_case(layout, W.DT_BF16, D, split, lambda t: 9.0 if t == split // 2 + 13 else -128.0, lambda t: 2.0 ** 60 * (1 + t % 2))
+    step.run()
+    assert_rows(step.result(), bc, oracle_out(bc), layout)
+
+
 @pytest.mark.parametrize("layout", list(LAYOUTS))
 @pytest.mark.parametrize("dtype,k_power,v_power", [
-    (W.DT_BF16, 0, -100), (W.DT_BF16, 0, 80), (W.DT_BF16, 60, 0), (W.DT_BF16, -60, -70), (W.DT_F16, 0, -10), (W.DT_F16, 0, 12), (W.DT_F16, 6, 3),
+    (W.DT_BF16, 0, -100), (W.DT_BF16, 0, -111), (W.DT_BF16, 0, 80), (W.DT_BF16, 60, 0), (W.DT_BF16, -60, -70), (W.DT_F16, 0, -10), (W.DT_F16, 0, 12), (W.DT_F16, 6, 3),
     (W.DT_F16, -6, 0),
 ])
 def test_keys_and_values_far_from_one(layout, dtype, k_power, v_power):
