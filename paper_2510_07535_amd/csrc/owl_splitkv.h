@@ -51,6 +51,7 @@
 // Only 32-key steps that reach past the prefix take the masked ("careful") path.
 #pragma once
 
+#include <float.h>
 #include <hip/hip_ext.h>
 
 #include <type_traits>
@@ -1438,8 +1439,10 @@ __device__ __forceinline__ void run_piece(const Params &launch_args, unsigned ch
                         O[t][u][r] *= inv_l;
                         big = fmaxf(big, fabsf(O[t][u][r]));
                     }
-                big = quad_column_max(big);                             // over the four lanes that hold this row
-                const float inv_s = big > 0.f ? 1.0f / big : 0.f;
+                // over the four lanes that hold this row; at least the least normal number (the inverse of subnormal means may be infinite,
+                // which made their answers no numbers; a row of zeros stays one)
+                big = fmaxf(quad_column_max(big), FLT_MIN);
+                const float inv_s = 1.0f / big;
                 uint4 *po = static_cast<uint4 *>(p.part_o) + slot * (size_t)(NT / 2 * 64) + lane;
 #pragma unroll
                 for (int u = 0; u < NT; u += 2)

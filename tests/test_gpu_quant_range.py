@@ -150,3 +150,14 @@ def test_values_of_zero(layout):
     step = make_step(bc, announced, split)
     step.run()
     assert not step.result().any() and step.flags() == 0
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_answers_below_the_least_normal_number(layout):
+    """Values of a few of the smallest steps that a block has, 2^-126, of both signs: their means are subnormal in 32 bits."""
+    n, group, hkv, batch, announced, split = LAYOUTS[layout]
+    case = W.make_case("least", 13, dtype=W.DT_BF16, Hq=hkv * group, Hkv=hkv, D=128, ctx_lens=[2 * split + 77] * batch, trees=[W.chain_tree(n)] * batch)
+    bc = make_blocks(case, W.widen(case.k_pool, W.DT_BF16), W.widen(case.v_pool, W.DT_BF16) * 2.0 ** -125)
+    step = make_step(bc, announced, split)
+    step.run()
+    assert_rows(step.result(), bc, oracle_out(bc), layout)
