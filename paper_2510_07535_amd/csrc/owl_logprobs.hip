@@ -1,10 +1,12 @@
 // Log probabilities of given tokens, entropy and the top alternatives of rows of logits.
 //
-// With x = scale * logit, m = max x, l = sum e^(x - m), t = sum (x - m) e^(x - m):
-//     log p = x - m - ln l,      entropy = ln l - t / l .
+// With x = scale * (logit - top), top the row's greatest logit, l = sum e^x, t = sum x e^x:
+//     log p = x - ln l,      entropy = ln l - t / l .
+// The greatest logit is kept as it is: times the scale it would round, by up to 2^-24 of itself, which every log probability would be
+// off by (that of a near-certain token above 0), and at the ends of the type it would be infinite.
 // A workgroup reads its logits once, into registers: a whole row of up to 32K, or a slice of 4K of a longer one (or of more rows than
-// there are compute units). A second launch, a workgroup a row, joins the slices' (m, l, t),
-//     M = max m_s,  w_s = e^(m_s - M),  L = sum w_s l_s,  T = sum w_s (t_s + (m_s - M) l_s) .
+// there are compute units). A second launch, a workgroup a row, joins the slices' (top, l, t),
+//     top = max top_s,  x_s = scale * (top_s - top),  w_s = e^x_s,  L = sum w_s l_s,  T = sum w_s (t_s + x_s l_s) .
 //
 // The greatest n logits: the threads form 64 groups; the n-th greatest of the groups' greatest is a bound that n logits reach, and if
 // the great ones lie in no order hardly more do (10: 11, 32: 44).  Those go to LDS, and one's place is the number of greater ones, of
@@ -137,9 +139,16 @@ __device__ __forceinline__ int greater_keys(const uint64_t *list, int count, uin
 template <typename T>
 __device__ __forceinline__ float to_float(T x) { return (float)x; }
 
-// What a slice leaves: its statistics; m is +infinity where it met a logit that is +infinity or no number.
+// scale * (x - y) for y >= x.  Of logits more than the greatest number apart the difference is formed of their halves.
+__device__ __forceinline__ float scaled_difference(float x, float y, float scale)
+{
+    const float d = x - y;
+    return d > -INFINITY ? d * scale : (0.5f * x - 0.5f * y) * scale * 2.0f;
+}
+
+// What a slice leaves: its statistics; top is +infinity where it met a logit that is +infinity or no number.
 struct SliceStats {
-    float m, l, t, unused;
+    float top, l, t, unused;
 };
 
 template <typename T>
@@ -180,16 +189,16 @@ template <typename T>
 struct Row {
     const LogArgs<T> &p;
     int r;
-    float m, log_l;
+    float top, log_l;
     bool bad;
 
-    __device__ Row(const LogArgs<T> &args, int row, int tid, float m_, float l, float t, const Given &given) : p(args), r(row), m(m_)
+    __device__ Row(const LogArgs<T> &args, int row, int tid, float top_, float l, float t, const Given &given) : p(args), r(row), top(top_)
     {
-        bad = m == INFINITY;
+        bad = top == INFINITY;
         log_l = logf(l);
         if (tid == 0) {
             if (bad) flag_status(p.status, OWL_DEV_BAD_LOGIT);
-            if (p.entropy) p.entropy[r] = bad ? __builtin_nanf("") : (m == -INFINITY ? 0.f : log_l - t / l);
+            if (p.entropy) p.entropy[r] = bad ? __builtin_nanf("") : (top == -INFINITY ? 0.f : log_l - t / l);
         }
         if (tid < p.n_given) {
             if (!given.known && given.token != -1) flag_status(p.status, OWL_DEV_BAD_TOKEN);
@@ -199,7 +208,7 @@ struct Row {
     __device__ float logp(float x) const
     {
         if (bad) return __builtin_nanf("");
-        return x > -INFINITY ? __builtin_fmaf(x, p.scale, -m) - log_l : -INFINITY;
+        return x > -INFINITY ? scaled_difference(x, top, p.scale) - log_l : -INFINITY;
     }
     __device__ void put(int j, uint64_t key) const
     {
@@ -265,8 +274,8 @@ __global__ void __launch_bounds__(64 * kWaves) logprob_slice_kernel(const LogArg
     float m = s_m[0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w]);
-    const float to_log2 = fminf(p.scale * kLog2e, FLT_MAX), base = m > -INFINITY ? m : 0.f;
-    m *= p.scale;
+    // (halves: their difference is finite, and rounded as the whole one)
+    const float to_log2 = fminf(p.scale * (2.0f * kLog2e), FLT_MAX), half_base = m > -INFINITY ? 0.5f * m : 0.f;
     float l = 0.f, t = 0.f;
 #pragma unroll
     for (int k = 0; k < kHeld; k += 4) {             // (four at a time: an exponential's result is waited for)
@@ -274,7 +283,7 @@ __global__ void __launch_bounds__(64 * kWaves) logprob_slice_kernel(const LogArg
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             // (maximum keeps what is no number, and the sums tell)
-            y[i] = __builtin_elementwise_maximum((x[k + i] - base) * to_log2, kFloor);
+            y[i] = __builtin_elementwise_maximum(__builtin_fmaf(x[k + i], 0.5f, -half_base) * to_log2, kFloor);
             e[i] = __builtin_amdgcn_exp2f(y[i]);
         }
         l += (e[0] + e[1]) + (e[2] + e[3]);
@@ -320,7 +329,7 @@ __global__ void __launch_bounds__(64 * kWaves) logprob_slice_kernel(const LogArg
         t += s_t[w];
     }
     t *= 1.0f / kLog2e;
-    if (!(l < INFINITY)) m = INFINITY;
+    if (!(l < INFINITY)) m = INFINITY;               // (one that is infinite less itself is no number either)
     auto list = [&](auto &&put) {                    // put(j, key): the slice's j-th greatest, in any order of j
         if (n_top == 0) return;
         const int found = s_found;
@@ -380,7 +389,7 @@ __global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(const LogArg
     const uint64_t column_key = holds ? all[(tid - column * slices) * n_top + column] : 0;
     const uint64_t first_key = tid < count ? all[tid] : 0;
     const Given given = take_given(p, r, tid);
-    const float wm = wave_fmax(mine.m);
+    const float wm = wave_fmax(mine.top);
     if (lane == 0) s_m[wave] = wm;
     if (tid == 0) {
         s_least = 1;
@@ -392,7 +401,7 @@ __global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(const LogArg
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w]);
     // (of rows without any logit, or with bad ones, the sums are not used)
-    const float d = m > -INFINITY ? fmaxf(mine.m - m, kFloor) : 0.f, weight = __builtin_amdgcn_exp2f(d * kLog2e);
+    const float d = m > -INFINITY ? fmaxf(scaled_difference(mine.top, m, p.scale), kFloor) : 0.f, weight = __builtin_amdgcn_exp2f(d * kLog2e);
     float l = weight * mine.l, t = weight * __builtin_fmaf(d, mine.l, mine.t);
     wave_sums(l, t);
     if (lane == 0) {
