@@ -66,7 +66,7 @@ typedef enum owl_dtype {
 #define OWL_DEV_BAD_CTX_LEN 4u  /* some ctx_lens[b] not in [0, max_ctx_len]       */
 #define OWL_DEV_BAD_ACCEPT 8u   /* accepted[] not a strictly increasing list in [0, n_draft) */
 #define OWL_DEV_BAD_NDRAFT 16u  /* some n_draft_seq[b] not in [0, n_draft]        */
-#define OWL_DEV_BAD_TOKEN 32u   /* drafter cell: some tokens[r] not in [0, vocab)  */
+#define OWL_DEV_BAD_TOKEN 32u   /* drafter cell, token log probabilities: some token not in [0, vocab) */
 #define OWL_DEV_BAD_ROW 64u     /* drafter cell: some parent_row[r] not in [0, n_states) */
 #define OWL_DEV_BAD_LOGIT 128u  /* token log probabilities: some row has a logit that is +infinity or no number */
 
@@ -335,7 +335,8 @@ owl_status owl_commit_kv(const owl_verify_desc *desc, void *k_cache, void *v_cac
  *
  *   desc        batch, head counts, head_dim, paging, strides, max_ctx_len and
  *               qkv_dtype are used (any owl_dtype); n_draft is not
- *   n_tokens    >= 1, a drafted tree or a prompt of any length
+ *   n_tokens    >= 1, a drafted tree or a prompt; below 2^24 (2^28 - 30 in owl_append_kv_quant), else
+ *               OWL_ERR_UNSUPPORTED, as for more than 65535 sequences
  *   q, k_new, v_new   [B][n_tokens] tokens of [heads][D], contiguous channels
  *               and heads; *_stride elements from one token to the next (so the
  *               three may be parts of one fused projection); q may be NULL
@@ -452,7 +453,7 @@ owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void 
  * Sums are formed in float32, in an order that depends on the shape only.
  */
 typedef struct owl_logprob_desc {
-    int32_t rows, vocab;      /* >= 1; vocab <= 2^20                        */
+    int32_t rows, vocab;      /* >= 1; vocab <= 2^20; rows below 2^22, of vocab > 8185 below 2^23 (else OWL_ERR_UNSUPPORTED) */
     int32_t n_given, n_top;
     int32_t dtype;            /* owl_dtype of the logits                    */
     float scale;              /* one over the temperature; finite, positive */

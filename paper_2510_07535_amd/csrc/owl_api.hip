@@ -353,6 +353,7 @@ owl_status scratch_address(void **out)
 }
 
 constexpr int kMaxGrid = 65535;                 // workgroups along the second and third dimension of a grid
+constexpr int64_t kMaxThreads = 0xFFFFFFFF;     // threads along a dimension of a grid
 
 bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
 
@@ -740,6 +741,7 @@ static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc
     if (page_table && !n_new_seq && (int64_t)desc->max_pages_per_seq * kPage < (int64_t)desc->max_ctx_len + a->n_tokens)
         return OWL_ERR_INVALID_ARG;
     if (desc->batch > kMaxGrid || desc->n_kv_heads > kMaxGrid) return OWL_ERR_UNSUPPORTED;
+    if (append_threads(a->n_tokens, k_scale != nullptr) > kMaxThreads) return OWL_ERR_UNSUPPORTED;
     if (launch_append(*desc, *a, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
                       ctx_lens, n_new_seq, dev_status, static_cast<hipStream_t>(stream)) != hipSuccess)
         return OWL_ERR_HIP;
@@ -773,6 +775,7 @@ static owl_status check_logprob(const owl_logprob_desc *d)
     if (!(d->scale > 0.0f) || !isfinite(d->scale)) return OWL_ERR_INVALID_ARG;
     if (d->dtype != OWL_BF16 && d->dtype != OWL_F32 && d->dtype != OWL_F16) return OWL_ERR_UNSUPPORTED;
     if (d->n_given > 64 || d->n_top > 32 || d->vocab > (1 << 20)) return OWL_ERR_UNSUPPORTED;
+    if (logprob_threads(*d, device_cus()) > kMaxThreads) return OWL_ERR_UNSUPPORTED;
     return OWL_OK;
 }
 

@@ -433,6 +433,11 @@ static hipError_t launch_append_as(const AppendArgs &p, int B, bool pairs, bool 
     return hipGetLastError();
 }
 
+int64_t append_threads(int64_t n_tokens, bool quant)
+{
+    return (quant ? (n_tokens + 2 * kPage - 2) / kPage : n_tokens) * kAppendThreads;
+}
+
 hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const void *q, const void *k_new, const void *v_new,
                          const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
                          uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,

@@ -96,6 +96,9 @@ hipError_t launch_accept(const int32_t *tokens, const int32_t *parent, const int
 hipError_t launch_commit(const owl_verify_desc &d, void *k_cache, void *v_cache, const int32_t *page_table,
                          const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
                          int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
+// Threads along the first dimension of the greatest grid of a call.
+int64_t append_threads(int64_t n_tokens, bool quant);
+int64_t logprob_threads(const owl_logprob_desc &d, int n_cus);
 // Caches of 8-bit blocks: k_scale is null for a cache in qkv_dtype.
 hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const void *q, const void *k_new, const void *v_new,
                          const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,

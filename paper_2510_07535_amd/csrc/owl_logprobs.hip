@@ -459,6 +459,11 @@ size_t logprob_scratch_bytes(const owl_logprob_desc &d, int cus)
     return plan.slices == 1 ? 256 : (size_t)d.rows * plan.slices * (sizeof(SliceStats) + (size_t)d.n_top * sizeof(uint64_t));
 }
 
+int64_t logprob_threads(const owl_logprob_desc &d, int cus)
+{
+    return (int64_t)d.rows * (plan_of(d, cus).slices == 1 ? 64 * kRowWaves : kJoinThreads);
+}
+
 template <typename T>
 static hipError_t launch_logprobs_as(const owl_logprob_desc &d, const void *logits, const int32_t *tokens, float *logprob, float *entropy,
                                      int32_t *top_ids, float *top_logprobs, void *scratch, uint32_t *status, int cus, hipStream_t s)
