@@ -406,14 +406,15 @@ owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_des
  * OWL_BF16 or OWL_F16.  The arithmetic is that of owl_verify_attn on a 16-bit
  * cache that holds the same numbers.  n_draft_seq as in owl_verify_attn_ragged, or NULL.
  * The workspace is that of owl_verify_attn_quant_workspace_size, 256-byte
- * aligned.  owl_verify_attn_quant_init does what owl_verify_attn_init does,
- * for this call.
+ * aligned.  owl_verify_attn_quant_init and owl_verify_attn_quant_plan do what
+ * owl_verify_attn_init and owl_verify_attn_plan do, for this call.
  */
 owl_status owl_verify_attn_quant(const owl_verify_desc *desc, const void *q, const void *k_cache, const void *v_cache,
                                  const uint8_t *k_scale, const uint8_t *v_scale, const int32_t *page_table,
                                  const int32_t *ctx_lens, const int32_t *tree_parent, const int32_t *n_draft_seq,
                                  void *out, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream);
 owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, size_t *bytes);
+owl_status owl_verify_attn_quant_plan(const owl_verify_desc *desc, owl_plan *plan);
 owl_status owl_verify_attn_quant_init(const owl_verify_desc *desc);
 
 /*

@@ -38,7 +38,7 @@ EXPORTS = (
     "owl_drafter_tiled_weight_bytes", "owl_drafter_tile_weights",
     "owl_verify_attn_init", "owl_verify_attn_noalloc",
     "owl_append_kv", "owl_append_kv_quant", "owl_verify_attn_quant", "owl_verify_attn_quant_workspace_size",
-    "owl_verify_attn_quant_init", "owl_commit_kv_quant", "owl_token_logprobs", "owl_token_logprobs_workspace_size",
+    "owl_verify_attn_quant_plan", "owl_verify_attn_quant_init", "owl_commit_kv_quant", "owl_token_logprobs", "owl_token_logprobs_workspace_size",
     "owl_status_str", "owl_version",
 )
 # ... and in include/owl_probe.h (measurement and self-test aids)
@@ -198,6 +198,8 @@ def lib() -> ctypes.CDLL:
         l.owl_verify_attn_quant.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11 + [ctypes.c_size_t, vp, vp]
         l.owl_verify_attn_quant_workspace_size.restype = ctypes.c_int
         l.owl_verify_attn_quant_workspace_size.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(ctypes.c_size_t)]
+        l.owl_verify_attn_quant_plan.restype = ctypes.c_int
+        l.owl_verify_attn_quant_plan.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(Plan)]
         l.owl_verify_attn_quant_init.restype = ctypes.c_int
         l.owl_verify_attn_quant_init.argtypes = [ctypes.POINTER(VerifyDesc)]
         l.owl_commit_kv_quant.restype = ctypes.c_int
@@ -490,6 +492,12 @@ def owl_verify_attn_quant_workspace_size(desc: VerifyDesc) -> int:
     n = ctypes.c_size_t(0)
     _check(lib().owl_verify_attn_quant_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "owl_verify_attn_quant_workspace_size")
     return int(n.value)
+
+
+def owl_verify_attn_quant_plan(desc: VerifyDesc) -> Plan:
+    plan = Plan()
+    _check(lib().owl_verify_attn_quant_plan(ctypes.byref(desc), ctypes.byref(plan)), "owl_verify_attn_quant_plan")
+    return plan
 
 
 def owl_verify_attn_quant_init(desc: VerifyDesc) -> None:

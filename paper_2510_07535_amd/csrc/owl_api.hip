@@ -677,6 +677,16 @@ owl_status owl_verify_attn_quant(const owl_verify_desc *desc, const void *q, con
                        workspace_bytes, dev_status, stream, OWL_PHASE_ALL, nullptr, nullptr, k_scale, v_scale);
 }
 
+owl_status owl_verify_attn_quant_plan(const owl_verify_desc *desc, owl_plan *plan)
+{
+    if (!plan) return OWL_ERR_INVALID_ARG;
+    FullPlan fp;
+    const owl_status st = make_plan(desc, &fp, true);
+    if (st != OWL_OK) return st;
+    *plan = fp.pub;
+    return OWL_OK;
+}
+
 owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, size_t *bytes)
 {
     if (!bytes) return OWL_ERR_INVALID_ARG;
