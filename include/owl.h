@@ -178,7 +178,8 @@ owl_status owl_verify_attn(const owl_verify_desc *desc, const void *q, const voi
  * memory (owl_verify_attn_noalloc) is looked up.  Every entry point does this
  * by itself on first use; a caller who wants the FIRST call for a shape to be
  * legal inside a stream capture (where such calls are not allowed) calls this
- * beforehand, outside the capture.  Launches nothing.
+ * beforehand, outside the capture.  Launches nothing.  (Appending, committing and
+ * the log probabilities need no set-up: their first call may fall into a capture.)
  */
 owl_status owl_verify_attn_init(const owl_verify_desc *desc);
 

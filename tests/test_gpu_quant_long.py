@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import oracle
-from block_helpers import DEV, BlockCase, QuantStep, assert_attention, i32, rng
+from block_helpers import DEV, BlockCase, QuantStep, assert_attention, block_case, i32, oracle_out, rng
 from oracle import cache_blocks as C
 from paper_2510_07535_amd import binding as B
 from paper_2510_07535_amd import workloads as W
@@ -107,3 +107,23 @@ def test_shares_of_hundreds_of_stages(layout, dtype):
     assert (plan.kernel_variant, plan.tiles_per_wave, plan.row_groups) == (_variant(own, index, dtype, 128), tiles, groups)
     assert 1600 * 64 * groups // plan.n_workgroups >= 300          # stages of a worker
     _check(bc, step, layout)
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("n,tiles,groups", [(4, 1, 1), (7, 2, 1), (15, 2, 2)])
+def test_equal_splits_of_a_batch_with_keys_of_their_own(n, tiles, groups, dtype):
+    r = rng(n)
+    hkv, announced = 3, 20000 if dtype == W.DT_BF16 else None       # (four tiles in bf16: from 16K tokens on)
+    bc = block_case("own-split", n, dtype=dtype, Hq=4 * hkv, Hkv=hkv, D=128, ctx_lens=[700, 33, 0, 1500], trees=[W.random_tree(n, 5, r) for _ in range(4)])
+    for counts in (None, [n, 0, 1, n // 2]):
+        step = QuantStep(bc, counts=counts, split_tokens=192, max_ctx_len=announced)
+        if announced is not None:
+            table = np.full((4, (announced + n + 15) // 16), -1, np.int32)
+            table[:, :bc.case.page_table.shape[1]] = bc.case.page_table
+            step.table, step.desc.max_pages_per_seq = i32(table), table.shape[1]
+            step.workspace = torch.empty(B.owl_verify_attn_quant_workspace_size(step.desc), dtype=torch.uint8, device=DEV)
+        plan = B.owl_verify_attn_quant_plan(step.desc)
+        assert plan.kernel_variant >= 47 and (plan.tiles_per_wave, plan.row_groups, plan.split_tokens) == (tiles, groups, 192)
+        step.run()
+        assert_attention(step.result(), bc, oracle_out(bc, counts), str(counts))
+        assert step.flags() == 0
