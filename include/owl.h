@@ -404,8 +404,11 @@ owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_des
 
 /*
  * owl_verify_attn over a cache of 8-bit blocks; q in desc->qkv_dtype, which is
- * OWL_BF16 or OWL_F16.  The arithmetic is that of owl_verify_attn on a 16-bit
- * cache that holds the same numbers.  n_draft_seq as in owl_verify_attn_ragged, or NULL.
+ * OWL_BF16 or OWL_F16.  The products, types and sums are those of owl_verify_attn on
+ * a 16-bit cache that holds the same numbers; references and the order of sums differ, and
+ * with them the last bits.  fp16 queries, and calls with few rows, leave fp32 partials whether or not
+ * OWL_FLAG_FP32_PARTIALS asks for them.  In bf16 values (V) up to 2^80 are summed without overflow.
+ * n_draft_seq as in owl_verify_attn_ragged, or NULL.
  * The workspace is that of owl_verify_attn_quant_workspace_size, 256-byte
  * aligned.  owl_verify_attn_quant_init and owl_verify_attn_quant_plan do what
  * owl_verify_attn_init and owl_verify_attn_plan do, for this call.

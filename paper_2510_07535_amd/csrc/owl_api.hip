@@ -108,7 +108,10 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // ring guards its references, below 4 M 0.73-0.99, 4-5 M 0.99 and 1.06, 7.9 M 1.14; 1, 2, 3 and 4 tiles of 64K tokens, 8 heads, 0.74 0.78 0.96
     // 0.96.  In a batch nothing is left over for groups that read again: 16 sequences of 200-600, 500-2K, 2K-8K, 8K-64K, 64 of 500-2K and 4 of
     // 4K-20K, bf16, 1 tile 0.74 0.67 0.69 0.72 0.63 0.73, 2 0.86 0.85 0.74 0.74 0.79 0.87, 4 1.07 1.01 0.96 0.92 1.10 0.93, 5 1.23 1.16 1.10 1.13 1.31 1.03;
-    // fp16, 4 1.01 0.93 0.92 0.89 1.03 0.88, 5 1.13 0.99 0.94 0.92 1.15 0.86, 6 1.12 0.98 0.99 0.93 1.18 0.90, 7 (8K-64K) 1.20.
+    // fp16, 4 1.01 0.93 0.92 0.89 1.03 0.88, 5 1.13 0.99 0.94 0.92 1.15 0.86, 6 1.12 0.98 0.99 0.93 1.18 0.90, 7 (8K-64K) 1.20.  head_dim 64
+    // has the same borders: lone, up to four tiles 0.56-0.86; more, bf16, below 1.1 M 0.79-0.95, 1.1-1.6 M 0.99-1.14 (1 head 0.80), above 1.02-1.55;
+    // fp16, below 4 M 0.75-0.95 and 0.98, 4.8-7.8 M 1.14-1.23 (5.2 M 0.98); 16 sequences of 500-2K, 2K-8K, 8K-64K, bf16, 1 tile 0.64 0.55 0.52, 2 0.76 0.64 0.52, 4 0.93
+    // 0.87 0.79, 5 1.20 1.09 1.09; fp16, 4 0.90 0.81 0.72, 5 1.05 0.91 0.88, 6 1.03 0.91 0.87, 7 1.13 1.02 1.10.
     const bool fp16 = d->qkv_dtype == OWL_F16;
     const bool few = quant && (d->batch == 1 ? RT <= 4 || T * RT * d->n_kv_heads <= (fp16 ? 4000000 : 1100000)
                                              : RT <= (fp16 ? (d->max_ctx_len < 4096 ? 4 : 6) : (d->max_ctx_len < 16384 ? 2 : 4)));
@@ -256,7 +259,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // Workspace: the partials that are written, and never less than equal splits of half the planned size
     // would need for a batch (the planned size for one sequence).
     // (8-bit blocks: own keys leave fp32 partials; and with fp16 queries, whose answer keeps 11 bits, fp16 partials would cost as much as
-    // its own rounding, 3.4e-4 instead of 2.1e-4 in all, for 2.5 % of the time)
+    // its own rounding: 3.4e-4 off the exact answer instead of 2.9e-4, for 2.5 % of the time)
     fp->half_partials = d->qkv_dtype != OWL_F32 && !few && !(quant && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
     const size_t o_bytes = (size_t)d->head_dim * kRowTile * (fp->half_partials ? 2 : 4), ml_bytes = kPartMl * sizeof(float);
     auto bytes_of = [&](size_t slots, size_t unit) -> size_t { return align_up((size_t)d->n_kv_heads * slots * RT * unit, 256); };

@@ -44,7 +44,8 @@
 // A cache of 8-bit blocks (kQuant) goes through the same loops.  Its bytes travel as they are, half the traffic, each wavefront's
 // page and its scale into a part of LDS of its own, and a stage ahead of its use the wavefront turns its page into 16 bits,
 // scale applied, and puts it into the ring: a power of two times a number of three mantissa bits, exact in bf16 and, inside its
-// range, in fp16.  The results are those of a 16-bit cache that holds the same numbers.
+// range, in fp16.  From there on it is a 16-bit cache that holds the same numbers, but for the bf16 reference (kLift) and fp16's partials,
+// which stay in fp32.
 //
 // Visibility (Sec. 3.2.2, Decode Stage): every row sees the whole prefix; among
 // the drafts, row (i, .) sees node j iff j is on i's root path, i included.

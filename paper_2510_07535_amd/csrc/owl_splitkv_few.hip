@@ -71,7 +71,8 @@ __device__ __forceinline__ void reads_done()
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 
-// Transposing 64-bit LDS read of bytes (see the file comment for the lane mapping).
+// Transposing 64-bit LDS read of bytes: in a block of 16 lanes, lane i receives byte i % 8 of what lanes 2e + i / 8 (e = 0..7) point at,
+// one after the other.  With lane 2e + c pointing at channels 8c .. 8c + 7 of key e, lane i ends up with channel i of eight keys.
 __device__ __forceinline__ uint2 lds_read_tr8(const unsigned char *p)
 {
     typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -333,6 +334,7 @@ __device__ __forceinline__ void run_quant_piece(const QuantParams &p, unsigned c
                 s0[r] = fast_exp2(__builtin_fmaf(s0[r], c_log2, -m[t]));
                 s1[r] = fast_exp2(__builtin_fmaf(s1[r], c_log2, -m[t]));
             }
+            // (the matrix pipe takes 16-bit weights; the row sum adds the same rounded ones)
             pf[t] = make_uint4(pack2<T>(s0[0], s0[1]), pack2<T>(s0[2], s0[3]), pack2<T>(s1[0], s1[1]), pack2<T>(s1[2], s1[3]));
         }
         if (more) {
