@@ -408,6 +408,8 @@ owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_des
  * a 16-bit cache that holds the same numbers; references and the order of sums differ, and
  * with them the last bits.  fp16 queries, and calls with few rows, leave fp32 partials whether or not
  * OWL_FLAG_FP32_PARTIALS asks for them.  In bf16 values (V) up to 2^80 are summed without overflow.
+ * A key that is no number makes the answers of the rows that see it no numbers, a value that is
+ * none those of all rows of its sequence and KV head.
  * n_draft_seq as in owl_verify_attn_ragged, or NULL.
  * The workspace is that of owl_verify_attn_quant_workspace_size, 256-byte
  * aligned.  owl_verify_attn_quant_init and owl_verify_attn_quant_plan do what

@@ -161,3 +161,27 @@ def test_answers_below_the_least_normal_number(layout):
     step = make_step(bc, announced, split)
     step.run()
     assert_rows(step.result(), bc, oracle_out(bc), layout)
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_a_draft_key_that_is_no_number_stays_in_its_subtree(layout, D, dtype):
+    n, group, hkv, batch, announced, split = LAYOUTS[layout]
+    r = rng(n + D)
+    tree = W.random_tree(n, 4, r)
+    case = W.make_case("nan", 14, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=D, ctx_lens=[split + 200] * batch, trees=[tree] * batch)
+    bc = make_blocks(case, W.widen(case.k_pool, dtype), W.widen(case.v_pool, dtype))
+    want, node = oracle_out(bc), n // 2
+    step = make_step(bc, announced, split)
+    page, slot = int(case.page_table[0, (split + 200 + node) // 16]), (split + 200 + node) % 16
+    for g in range(hkv):
+        step.k[bc.k._at(page, g, slot).start + 7] = NAN_BYTE
+    step.run()
+    got = step.result()
+    sees = np.zeros(n, bool)
+    for i in range(n):
+        sees[i] = i == node or (tree[i] >= 0 and sees[tree[i]])
+    assert sees.any() and not sees.all() and np.isnan(got[0, sees]).all()
+    got[0, sees] = want[0, sees]
+    assert_attention(got, bc, want, layout)
