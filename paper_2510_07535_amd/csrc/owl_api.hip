@@ -112,6 +112,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // has the same borders: lone, up to four tiles 0.56-0.86; more, bf16, below 1.1 M 0.79-0.95, 1.1-1.6 M 0.99-1.14 (1 head 0.80), above 1.02-1.55;
     // fp16, below 4 M 0.75-0.95 and 0.98, 4.8-7.8 M 1.14-1.23 (5.2 M 0.98); 16 sequences of 500-2K, 2K-8K, 8K-64K, bf16, 1 tile 0.64 0.55 0.52, 2 0.76 0.64 0.52, 4 0.93
     // 0.87 0.79, 5 1.20 1.09 1.09; fp16, 4 0.90 0.81 0.72, 5 1.05 0.91 0.88, 6 1.03 0.91 0.87, 7 1.13 1.02 1.10.
+    // (Within the ring, 8-bit blocks have the tiles, row groups and pairs that were measured for 16-bit caches.)
     const bool fp16 = d->qkv_dtype == OWL_F16;
     const bool few = quant && (d->batch == 1 ? RT <= 4 || T * RT * d->n_kv_heads <= (fp16 ? 4000000 : 1100000)
                                              : RT <= (fp16 ? (d->max_ctx_len < 4096 ? 4 : 6) : (d->max_ctx_len < 16384 ? 2 : 4)));
