@@ -1,10 +1,10 @@
 """Operators of a decoding loop over a cache of 4-bit groups, as cases that can be timed, each with a plain form in torch.
 
   norm      new rows go into the paged cache, the heads of q and k normalised and rotated on the way (``owl_append_kv_norm``)
-  append    the same into a cache of 4-bit groups, with or without the norms (``owl_append_kv_quant4``)
-  verify    the verify-step attention over such a cache (``owl_verify_attn_quant4``)
-  commit    the accepted rows of such a cache move behind the context (``owl_commit_kv_quant4``)
-  gather    cached rows are read back as 16-bit numbers (``owl_gather_kv_quant4``)
+  append    the same into a cache of 4-bit groups, with or without the norms (``owl_append_kv_groups``)
+  verify    the verify-step attention over such a cache (``owl_verify_attn_groups``)
+  commit    the accepted rows of such a cache move behind the context (``owl_commit_kv_groups``)
+  gather    cached rows are read back as 16-bit numbers (``owl_gather_kv_groups``)
 
 A group is 32 neighbouring channels of one token and KV head, of K or of V: 32 e2m1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign), two
 a byte, the lower channel in the lower half, and one scale byte s; a value is e2m1 * 2^(s - 127), and s = 255 says that the group
@@ -418,7 +418,7 @@ def _kept(s):
         return B, desc, torch.empty_like(s["lens"])
     if kind == "gather":
         return B, desc, *(torch.empty((n, hkv, d), dtype=_TORCH[case["dtype"]], device=DEV) for _ in range(2))
-    return B, desc, torch.empty_like(s["q"]), torch.empty(B.owl_verify_attn_quant4_workspace_size(desc), dtype=torch.uint8, device=DEV)
+    return B, desc, torch.empty_like(s["q"]), torch.empty(B.owl_verify_attn_groups_workspace_size(desc), dtype=torch.uint8, device=DEV)
 
 
 def _own_run(s):
@@ -435,20 +435,20 @@ def _own_run(s):
             B.owl_append_kv_norm(desc, app, norm, q, k, v, s["q_gain"], s["k_gain"], freq, s["pos"], q_out, s["k"], s["v"], None, None,
                                  s["table"], s["lens"], None, s["status"])
             return {"q": q_out, "k": s["k"], "v": s["v"]}
-        B.owl_append_kv_quant4(desc, app, norm, q, k, v, s["q_gain"], s["k_gain"], freq, s["pos"], q_out, s["k"], s["v"], s["k_scale"],
+        B.owl_append_kv_groups(desc, app, norm, q, k, v, s["q_gain"], s["k_gain"], freq, s["pos"], q_out, s["k"], s["v"], s["k_scale"],
                                s["v_scale"], s["table"], s["lens"], None, s["status"])
         return {"q": q_out, "k": s["k"], "v": s["v"], "k_scale": s["k_scale"], "v_scale": s["v_scale"]}
     if kind == "commit":
         B, desc, new_lens = s["kept"]
-        B.owl_commit_kv_quant4(desc, s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["lens"], s["accepted"], s["count"], new_lens, s["status"])
+        B.owl_commit_kv_groups(desc, s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["lens"], s["accepted"], s["count"], new_lens, s["status"])
         return {"k": s["k"], "v": s["v"], "k_scale": s["k_scale"], "v_scale": s["v_scale"], "lens": new_lens}
     if kind == "gather":
         B, desc, k, v = s["kept"]
-        B.owl_gather_kv_quant4(desc, s["k"], s["k_scale"], s["table"], 0, case["ctx_lo"], case["n"], k, s["status"])
-        B.owl_gather_kv_quant4(desc, s["v"], s["v_scale"], s["table"], 0, case["ctx_lo"], case["n"], v, s["status"])
+        B.owl_gather_kv_groups(desc, s["k"], s["k_scale"], s["table"], 0, case["ctx_lo"], case["n"], k, s["status"])
+        B.owl_gather_kv_groups(desc, s["v"], s["v_scale"], s["table"], 0, case["ctx_lo"], case["n"], v, s["status"])
         return {"k": k, "v": v}
     B, desc, out, workspace = s["kept"]
-    B.owl_verify_attn_quant4(desc, s["q"], s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["lens"], s["parent"], s["counts"], out,
+    B.owl_verify_attn_groups(desc, s["q"], s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], s["lens"], s["parent"], s["counts"], out,
                              workspace, s["status"])
     return {"out": out}
 
