@@ -435,6 +435,64 @@ owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void 
                                uint32_t *dev_status, void *stream);
 
 /*
+ * Norms of the heads on the way: owl_append_kv with every head of q and of k_new first divided by its root mean square,
+ *     x -> x / sqrt(mean of x^2 over the D channels + eps) * gain[channel] ,
+ * then rotated; norms and rotation in 64 bits, rounded once to qkv_dtype.  Values (V) are stored as they come.
+ *   norm        eps >= 0, finite
+ *   q_gain, k_gain   [D] float32 each, the same for all heads of q and of k, or NULL (1)
+ *   k_scale, v_scale   NULL: a cache in qkv_dtype, as owl_append_kv; both given: a cache of 8-bit blocks, as owl_append_kv_quant
+ * All else as in those.  A row with a number that is infinite or none comes out with what the formula gives for it.
+ */
+typedef struct owl_norm_desc {
+    float eps;
+} owl_norm_desc;
+
+owl_status owl_append_kv_norm(const owl_verify_desc *desc, const owl_append_desc *append, const owl_norm_desc *norm, const void *q,
+                              const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                              const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                              const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status,
+                              void *stream);
+
+/*
+ * Caches of 4-bit groups.  A group is 32 neighbouring channels of one token and KV head, of K or of V: 32 e2m1 codes (a sign, two
+ * exponent bits and one mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6), two a byte, the lower channel in the lower half, and
+ * one scale byte s.  A cached number is
+ *     e2m1(code) * 2^(s - 127)
+ * in qkv_dtype, which is OWL_BF16 or OWL_F16 here; s = 255 says that the group is no numbers, and its codes are 0.  A row of D channels takes D / 2 bytes; in a
+ * descriptor for such a cache the kv strides count bytes, are multiples of 16, and kv_stride_token is at most 2^26.  The scale bytes are
+ * k_scale and v_scale [n_pool_pages][Hkv][16][D / 32], contiguous, 16-byte aligned.  A quarter of a 16-bit cache's memory and
+ * traffic (17/64).  A group's scale is
+ *     the least e in [e0, e1] with  max |number| <= 7 * 2^e ,    s = e + 127 ,
+ * e0 = -125, e1 = 125 (OWL_BF16) or -23, 13 (OWL_F16), and its numbers are rounded to nearest even, those beyond 6 * 2^e to that: up to
+ * 7 * 2^e none is off by more than half a step.  A group with a number that is infinite or none becomes no numbers.
+ * Groups ask nothing of other tokens: rows are written, moved and read one by one, and moving a row leaves it as it is.
+ *
+ * owl_append_kv_groups: the rows that owl_append_kv (norm NULL; the gains too) or owl_append_kv_norm would store are what is rounded
+ * to 4 bits.  n_tokens is below 2^24, else OWL_ERR_UNSUPPORTED.  All else as in those.
+ */
+owl_status owl_append_kv_groups(const owl_verify_desc *desc, const owl_append_desc *append, const owl_norm_desc *norm, const void *q,
+                                const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                                const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status,
+                                void *stream);
+
+/*
+ * owl_commit_kv in a cache of 4-bit groups: rows move with their scales, bit for bit.  All else as owl_commit_kv; page_table may be
+ * NULL only if batch is 1.
+ */
+owl_status owl_commit_kv_groups(const owl_verify_desc *desc, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
+                                int32_t *new_ctx_lens, uint32_t *dev_status, void *stream);
+
+/*
+ * Reading back: n_tokens rows of sequence `seq`, from logical position first_pos on, of `cache` (K or V) with its scales, into
+ * dst[n_tokens][Hkv][D] in qkv_dtype, exactly what the groups stand for (no numbers where s is 255).  Positions and counts up to 2^32; page_table may be NULL only if batch is
+ * 1; a bad page reads page 0 (OWL_DEV_BAD_PAGE).  dst overlaps nothing else.
+ */
+owl_status owl_gather_kv_groups(const owl_verify_desc *desc, const void *cache, const uint8_t *scale, const int32_t *page_table,
+                                int32_t seq, int64_t first_pos, int64_t n_tokens, void *dst, uint32_t *dev_status, void *stream);
+
+/*
  * What a row of logits says about its tokens (Sec. 2: the target's own next
  * tokens are what drafts are checked against; Sec. 3.2.1: a node's likeliest
  * tokens become its children).  For every row r, with x = scale * logits[r],

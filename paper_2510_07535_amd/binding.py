@@ -39,6 +39,7 @@ EXPORTS = (
     "owl_verify_attn_init", "owl_verify_attn_noalloc",
     "owl_append_kv", "owl_append_kv_quant", "owl_verify_attn_quant", "owl_verify_attn_quant_workspace_size",
     "owl_verify_attn_quant_plan", "owl_verify_attn_quant_init", "owl_commit_kv_quant", "owl_token_logprobs", "owl_token_logprobs_workspace_size",
+    "owl_append_kv_norm", "owl_append_kv_groups", "owl_commit_kv_groups", "owl_gather_kv_groups",
     "owl_status_str", "owl_version",
 )
 # ... and in include/owl_probe.h (measurement and self-test aids)
@@ -96,6 +97,11 @@ class AppendDesc(ctypes.Structure):
         ("n_tokens", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("rot_style", ctypes.c_int32), ("rot_scale", ctypes.c_float),
         ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
     ]
+
+
+class NormDesc(ctypes.Structure):
+    """Mirror of owl_norm_desc."""
+    _fields_ = [("eps", ctypes.c_float)]
 
 
 class LogprobDesc(ctypes.Structure):
@@ -204,6 +210,14 @@ def lib() -> ctypes.CDLL:
         l.owl_verify_attn_quant_init.argtypes = [ctypes.POINTER(VerifyDesc)]
         l.owl_commit_kv_quant.restype = ctypes.c_int
         l.owl_commit_kv_quant.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11
+        l.owl_append_kv_norm.restype = ctypes.c_int
+        l.owl_append_kv_norm.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(AppendDesc), ctypes.POINTER(NormDesc)] + [vp] * 17
+        l.owl_append_kv_groups.restype = ctypes.c_int
+        l.owl_append_kv_groups.argtypes = l.owl_append_kv_norm.argtypes
+        l.owl_commit_kv_groups.restype = ctypes.c_int
+        l.owl_commit_kv_groups.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11
+        l.owl_gather_kv_groups.restype = ctypes.c_int
+        l.owl_gather_kv_groups.argtypes = [ctypes.POINTER(VerifyDesc), vp, vp, vp, i32, i64, i64, vp, vp, vp]
         l.owl_token_logprobs.restype = ctypes.c_int
         l.owl_token_logprobs.argtypes = [ctypes.POINTER(LogprobDesc)] + [vp] * 7 + [ctypes.c_size_t, vp, vp]
         l.owl_token_logprobs_workspace_size.restype = ctypes.c_int
@@ -530,6 +544,63 @@ def owl_commit_kv_quant(desc: VerifyDesc, k_cache, v_cache, k_scale, v_scale, pa
         _stream() if stream is None else stream)
     if rc != OWL_OK:
         raise OwlError(rc, "owl_commit_kv_quant")
+
+
+def owl_append_kv_norm(desc: VerifyDesc, append: AppendDesc, norm, q, k_new, v_new, q_gain, k_gain, inv_freq, pos_ids, q_out, k_cache, v_cache,
+                       k_scale, v_scale, page_table, ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
+    """owl_append_kv with norms of the heads; k_scale and v_scale are None, or those of a cache of 8-bit blocks."""
+    rc = lib().owl_append_kv_norm(
+        ctypes.byref(desc), ctypes.byref(append), None if norm is None else ctypes.byref(norm), None if q is None else q.data_ptr(),
+        None if k_new is None else k_new.data_ptr(), None if v_new is None else v_new.data_ptr(),
+        None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+        None if inv_freq is None else inv_freq.data_ptr(), None if pos_ids is None else pos_ids.data_ptr(),
+        None if q_out is None else q_out.data_ptr(), None if k_cache is None else k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+        None if v_scale is None else v_scale.data_ptr(), None if page_table is None else page_table.data_ptr(),
+        None if ctx_lens is None else ctx_lens.data_ptr(), None if n_new_seq is None else n_new_seq.data_ptr(),
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_append_kv_norm")
+
+
+def owl_append_kv_groups(desc: VerifyDesc, append: AppendDesc, norm, q, k_new, v_new, q_gain, k_gain, inv_freq, pos_ids, q_out, k_cache, v_cache,
+                         k_scale, v_scale, page_table, ctx_lens, n_new_seq=None, dev_status=None, stream: Optional[int] = None) -> None:
+    """Append to a cache of 4-bit groups (uint8 pools [..., D / 2], uint8 scales [n_pool_pages][Hkv][16][D / 32]); norm may be None."""
+    rc = lib().owl_append_kv_groups(
+        ctypes.byref(desc), ctypes.byref(append), None if norm is None else ctypes.byref(norm), None if q is None else q.data_ptr(),
+        None if k_new is None else k_new.data_ptr(), None if v_new is None else v_new.data_ptr(),
+        None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+        None if inv_freq is None else inv_freq.data_ptr(), None if pos_ids is None else pos_ids.data_ptr(),
+        None if q_out is None else q_out.data_ptr(), None if k_cache is None else k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+        None if v_scale is None else v_scale.data_ptr(), None if page_table is None else page_table.data_ptr(),
+        None if ctx_lens is None else ctx_lens.data_ptr(), None if n_new_seq is None else n_new_seq.data_ptr(),
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_append_kv_groups")
+
+
+def owl_commit_kv_groups(desc: VerifyDesc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,
+                         new_ctx_lens=None, dev_status=None, stream: Optional[int] = None) -> None:
+    rc = lib().owl_commit_kv_groups(
+        ctypes.byref(desc), None if k_cache is None else k_cache.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
+        None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
+        None if page_table is None else page_table.data_ptr(), None if ctx_lens is None else ctx_lens.data_ptr(),
+        None if accepted is None else accepted.data_ptr(), None if n_accept is None else n_accept.data_ptr(),
+        None if new_ctx_lens is None else new_ctx_lens.data_ptr(), None if dev_status is None else dev_status.data_ptr(),
+        _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_commit_kv_groups")
+
+
+def owl_gather_kv_groups(desc: VerifyDesc, cache, scale, page_table, seq: int, first_pos: int, n_tokens: int, dst, dev_status=None,
+                         stream: Optional[int] = None) -> None:
+    rc = lib().owl_gather_kv_groups(
+        ctypes.byref(desc), None if cache is None else cache.data_ptr(), None if scale is None else scale.data_ptr(),
+        None if page_table is None else page_table.data_ptr(), seq, first_pos, n_tokens, None if dst is None else dst.data_ptr(),
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_gather_kv_groups")
 
 
 def owl_token_logprobs_workspace_size(desc: LogprobDesc) -> int:

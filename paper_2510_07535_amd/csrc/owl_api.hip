@@ -32,7 +32,8 @@ int device_cus()
     return n;
 }
 
-owl_status check_desc(const owl_verify_desc *d)
+// least_row: what a token of a head takes at least, in units of the strides.
+owl_status check_desc(const owl_verify_desc *d, int least_row = 0)
 {
     if (!d) return OWL_ERR_INVALID_ARG;
     if (d->batch < 1 || d->n_draft < 1 || d->n_q_heads < 1 || d->n_kv_heads < 1) return OWL_ERR_INVALID_ARG;
@@ -51,7 +52,7 @@ owl_status check_desc(const owl_verify_desc *d)
     const int64_t st[3] = {d->kv_stride_page, d->kv_stride_head, d->kv_stride_token};
     for (int64_t s : st)
         if (s < 0 || (s * es) % 16 != 0) return OWL_ERR_INVALID_ARG;
-    if (d->kv_stride_token < d->head_dim) return OWL_ERR_INVALID_ARG;
+    if (d->kv_stride_token < (least_row > 0 ? least_row : d->head_dim)) return OWL_ERR_INVALID_ARG;
     if ((int64_t)d->n_q_heads / d->n_kv_heads * d->n_draft > 64 * 64) return OWL_ERR_UNSUPPORTED;
     return OWL_OK;
 }
@@ -69,10 +70,10 @@ struct FullPlan {
     dim3 grid;                // of the split-KV pass
 };
 
-// What a descriptor for a cache of 8-bit blocks has to be beyond that: its kv strides count bytes.
-owl_status check_quant_desc(const owl_verify_desc *d)
+// What a descriptor for a cache of 8-bit blocks, or of 4-bit groups, has to be beyond that: its kv strides count bytes.
+owl_status check_quant_desc(const owl_verify_desc *d, Cached cached = Cached::kBlocks8)
 {
-    owl_status st = check_desc(d);
+    owl_status st = check_desc(d, d && cached == Cached::kGroups4 ? d->head_dim / 2 : 0);
     if (st != OWL_OK) return st;
     if (d->qkv_dtype == OWL_F32) return OWL_ERR_UNSUPPORTED;
     for (int64_t s : {d->kv_stride_page, d->kv_stride_head, d->kv_stride_token})
@@ -730,14 +731,54 @@ owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void 
     return OWL_OK;
 }
 
+// ---- caches of 4-bit groups ----
+owl_status owl_commit_kv_groups(const owl_verify_desc *desc, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
+                                int32_t *new_ctx_lens, uint32_t *dev_status, void *stream)
+{
+    const owl_status st = check_quant_desc(desc, Cached::kGroups4);
+    if (st != OWL_OK) return st;
+    if (!k_cache || !v_cache || !k_scale || !v_scale || !ctx_lens || !accepted || !n_accept) return OWL_ERR_INVALID_ARG;
+    if (new_ctx_lens == ctx_lens || (!page_table && desc->batch > 1)) return OWL_ERR_INVALID_ARG;
+    for (const void *ptr : {k_cache, v_cache, (void *)k_scale, (void *)v_scale})
+        if (misaligned(ptr, 16)) return OWL_ERR_INVALID_ARG;
+    if (desc->batch > kMaxGrid) return OWL_ERR_UNSUPPORTED;
+    if (page_table &&
+        (int64_t)desc->max_pages_per_seq * kPage < (int64_t)desc->max_ctx_len + desc->n_draft)
+        return OWL_ERR_INVALID_ARG;
+    if (launch_commit_groups(*desc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,
+                             new_ctx_lens, dev_status, static_cast<hipStream_t>(stream)) != hipSuccess)
+        return OWL_ERR_HIP;
+    return OWL_OK;
+}
+
+owl_status owl_gather_kv_groups(const owl_verify_desc *desc, const void *cache, const uint8_t *scale, const int32_t *page_table,
+                                int32_t seq, int64_t first_pos, int64_t n_tokens, void *dst, uint32_t *dev_status, void *stream)
+{
+    const owl_status st = check_quant_desc(desc, Cached::kGroups4);
+    if (st != OWL_OK) return st;
+    if (!cache || !scale || !dst || seq < 0 || seq >= desc->batch || first_pos < 0 || n_tokens < 0) return OWL_ERR_INVALID_ARG;
+    if (!page_table && desc->batch > 1) return OWL_ERR_INVALID_ARG;
+    if (misaligned(cache, 16) || misaligned(scale, 16) || misaligned(dst, 16)) return OWL_ERR_INVALID_ARG;
+    if (first_pos > ((int64_t)1 << 32) || n_tokens > ((int64_t)1 << 32)) return OWL_ERR_UNSUPPORTED;      // pages are numbered in 31 bits
+    if (launch_gather_groups(*desc, cache, scale, page_table, seq, first_pos, n_tokens, dst, dev_status,
+                             static_cast<hipStream_t>(stream)) != hipSuccess)
+        return OWL_ERR_HIP;
+    return OWL_OK;
+}
+
 // ---- new rows of the cache ----
-static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc *a, const void *q, const void *k_new,
-                              const void *v_new, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
+static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc *a, const owl_norm_desc *norm, Cached cached,
+                              const void *q, const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
                               void *v_cache, uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table,
                               const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status, void *stream)
 {
-    const owl_status st = k_scale ? check_quant_desc(desc) : check_desc(desc);
+    const owl_status st = cached == Cached::kOwnType ? check_desc(desc) : check_quant_desc(desc, cached);
     if (st != OWL_OK) return st;
+    if (norm && (!(norm->eps >= 0.0f) || !isfinite(norm->eps))) return OWL_ERR_INVALID_ARG;
+    if (!norm && (q_gain || k_gain)) return OWL_ERR_INVALID_ARG;
+    if (misaligned(q_gain, 4) || misaligned(k_gain, 4)) return OWL_ERR_INVALID_ARG;
+    if (cached == Cached::kGroups4 && (misaligned(k_scale, 16) || misaligned(v_scale, 16))) return OWL_ERR_INVALID_ARG;
     if (!a || !k_new || !v_new || !k_cache || !v_cache || !ctx_lens) return OWL_ERR_INVALID_ARG;
     if ((q == nullptr) != (q_out == nullptr) || (!page_table && desc->batch > 1)) return OWL_ERR_INVALID_ARG;
     if (a->n_tokens < 1 || a->n_tokens > (1 << 30)) return OWL_ERR_INVALID_ARG;
@@ -755,8 +796,8 @@ static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc
     if (page_table && !n_new_seq && (int64_t)desc->max_pages_per_seq * kPage < (int64_t)desc->max_ctx_len + a->n_tokens)
         return OWL_ERR_INVALID_ARG;
     if (desc->batch > kMaxGrid || desc->n_kv_heads > kMaxGrid) return OWL_ERR_UNSUPPORTED;
-    if (append_threads(a->n_tokens, k_scale != nullptr) > kMaxThreads) return OWL_ERR_UNSUPPORTED;
-    if (launch_append(*desc, *a, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
+    if (append_threads(a->n_tokens, cached) > kMaxThreads) return OWL_ERR_UNSUPPORTED;
+    if (launch_append(*desc, *a, norm, cached, q, k_new, v_new, q_gain, k_gain, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
                       ctx_lens, n_new_seq, dev_status, static_cast<hipStream_t>(stream)) != hipSuccess)
         return OWL_ERR_HIP;
     return OWL_OK;
@@ -767,8 +808,8 @@ owl_status owl_append_kv(const owl_verify_desc *desc, const owl_append_desc *app
                          void *v_cache, const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq,
                          uint32_t *dev_status, void *stream)
 {
-    return append_impl(desc, append, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, nullptr, nullptr, page_table,
-                       ctx_lens, n_new_seq, dev_status, stream);
+    return append_impl(desc, append, nullptr, Cached::kOwnType, q, k_new, v_new, nullptr, nullptr, inv_freq, pos_ids, q_out, k_cache, v_cache,
+                       nullptr, nullptr, page_table, ctx_lens, n_new_seq, dev_status, stream);
 }
 
 owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_desc *append, const void *q, const void *k_new,
@@ -777,8 +818,30 @@ owl_status owl_append_kv_quant(const owl_verify_desc *desc, const owl_append_des
                                const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status, void *stream)
 {
     if (!k_scale || !v_scale) return OWL_ERR_INVALID_ARG;
-    return append_impl(desc, append, q, k_new, v_new, inv_freq, pos_ids, q_out, k_cache, v_cache, k_scale, v_scale, page_table,
-                       ctx_lens, n_new_seq, dev_status, stream);
+    return append_impl(desc, append, nullptr, Cached::kBlocks8, q, k_new, v_new, nullptr, nullptr, inv_freq, pos_ids, q_out, k_cache, v_cache,
+                       k_scale, v_scale, page_table, ctx_lens, n_new_seq, dev_status, stream);
+}
+
+owl_status owl_append_kv_norm(const owl_verify_desc *desc, const owl_append_desc *append, const owl_norm_desc *norm, const void *q,
+                              const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                              const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                              const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status,
+                              void *stream)
+{
+    if (!norm || (k_scale == nullptr) != (v_scale == nullptr)) return OWL_ERR_INVALID_ARG;
+    return append_impl(desc, append, norm, k_scale ? Cached::kBlocks8 : Cached::kOwnType, q, k_new, v_new, q_gain, k_gain, inv_freq, pos_ids,
+                       q_out, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, n_new_seq, dev_status, stream);
+}
+
+owl_status owl_append_kv_groups(const owl_verify_desc *desc, const owl_append_desc *append, const owl_norm_desc *norm, const void *q,
+                                const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                                const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status,
+                                void *stream)
+{
+    if (!k_scale || !v_scale) return OWL_ERR_INVALID_ARG;
+    return append_impl(desc, append, norm, Cached::kGroups4, q, k_new, v_new, q_gain, k_gain, inv_freq, pos_ids, q_out, k_cache, v_cache,
+                       k_scale, v_scale, page_table, ctx_lens, n_new_seq, dev_status, stream);
 }
 
 // ---- rows of logits ----

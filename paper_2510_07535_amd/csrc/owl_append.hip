@@ -1,5 +1,6 @@
-// New rows of the paged cache: appending keys and values with the rotary position embedding on the way, to a cache of
-// 16- or 32-bit numbers or of 8-bit blocks, and the commit of accepted rows in a cache of 8-bit blocks.
+// New rows of the paged cache: appending keys and values with the norms of the heads and the rotary position embedding on the
+// way, to a cache of 16- or 32-bit numbers, of 8-bit blocks or of 4-bit groups, and the commit of accepted rows in a cache of
+// 8-bit blocks.
 #include <type_traits>
 
 #include "owl_device.h"
@@ -112,7 +113,8 @@ struct AppendArgs {
     int64_t q_stride, k_stride, v_stride;                    // bytes between tokens
     int64_t stride_page, stride_head, stride_token, n_pool_pages;      // bytes; pages
     int32_t n, Hq, Hkv, rot_dim, max_pages, max_ctx_len;
-    float rot_scale;
+    float rot_scale, eps;
+    const float *q_gain, *k_gain;                            // norms: a gain a channel, or null = ones
 };
 
 // An item is two 16-byte pieces of a head that are turned together (or copied): item i < rot_dim / 2E holds the frequencies
@@ -141,6 +143,80 @@ __device__ __forceinline__ void turn(Piece<T> &a, Piece<T> &b, const double2 *cs
     }
 }
 
+// ---------------------------------------------------------------------------
+// The norm of a head, in 64 bits like the rotation behind it, so that a row is rounded once, when it is stored.  A head's items lie in
+// neighbouring lanes, whose squares meet by DPP, no LDS.
+// ---------------------------------------------------------------------------
+template <int ctrl>
+__device__ __forceinline__ double lane_of(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, ctrl, 0xf, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), ctrl, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Sum over n = 4, 8 or 16 neighbouring lanes, all of them active; each gets it, and the same one.
+template <int n>
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    v += lane_of<0xB1>(v);                                   // lane ^ 1
+    v += lane_of<0x4E>(v);                                   // lane ^ 2
+    if constexpr (n > 4) v += lane_of<0x141>(v);             // the other four of eight, mirrored
+    if constexpr (n > 8) v += lane_of<0x140>(v);             // the other eight of sixteen
+    return v;
+}
+
+// 1 / sqrt(x), to about 1e-16 of it: the instruction's 2^-26 or so and two Newton steps.  0 and infinity, for which the steps are
+// no numbers, keep what the instruction gives, infinity and 0.
+__device__ __forceinline__ double inverse_root(double x)
+{
+    const double y0 = __builtin_amdgcn_rsq(x);
+    double y = y0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+    return x > 0.0 && x < __builtin_inf() ? y : y0;
+}
+
+// An item of a head of q or k: normalised with the head's gains (of channels at.x .. and at.y ..), then turned if `rotate` says so,
+// and rounded once.  kItems lanes that hold the same head call this together.
+template <typename T, bool kPairs, int kItems>
+__device__ __forceinline__ void normalise(Piece<T> &a, Piece<T> &b, const float *gain, int2 at, double eps, bool rotate, const double2 *cs, int step)
+{
+    constexpr int E = Piece<T>::E;
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum = __builtin_fma((double)a.v[e], (double)a.v[e], __builtin_fma((double)b.v[e], (double)b.v[e], sum));
+    const double r = inverse_root(lanes_sum<kItems>(sum) * (1.0 / (2 * E * kItems)) + eps);
+    auto rounded = [](double d) -> float { return std::is_same<T, float>::value ? (float)d : to_odd(d); };
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        // the two channels that frequency E i + e turns, or channels e of the two pieces
+        float &x = kPairs ? (2 * e < E ? a.v[(2 * e) % E] : b.v[(2 * e) % E]) : a.v[e];
+        float &y = kPairs ? (2 * e < E ? a.v[(2 * e + 1) % E] : b.v[(2 * e + 1) % E]) : b.v[e];
+        const int cx = kPairs ? (2 * e < E ? at.x : at.y) + (2 * e) % E : at.x + e, cy = kPairs ? cx + 1 : at.y + e;
+        const double xd = (double)x * r * (double)gain[cx], yd = (double)y * r * (double)gain[cy];
+        double p = xd, q = yd;
+        if (rotate) {
+            const double2 w = cs[e * step];
+            p = xd * w.x - yd * w.y;
+            q = yd * w.x + xd * w.y;
+        }
+        x = rounded(p);
+        y = rounded(q);
+    }
+}
+
+// The gains of q, then of k, into LDS.
+template <int D, int kThreads>
+__device__ __forceinline__ void take_gains(const AppendArgs &p, float *s_gain)
+{
+    for (int c = threadIdx.x; c < 2 * D; c += kThreads) {
+        const float *from = c < D ? p.q_gain : p.k_gain;
+        s_gain[c] = from ? from[c % D] : 1.0f;
+    }
+}
+
 __device__ __forceinline__ uint4 load16(const unsigned char *p) { return *reinterpret_cast<const uint4 *>(p); }
 __device__ __forceinline__ void store16(unsigned char *p, const uint4 &x) { *reinterpret_cast<uint4 *>(p) = x; }
 
@@ -163,16 +239,88 @@ __device__ __forceinline__ int append_page(const AppendArgs &p, int b, int lp, b
     return -1;
 }
 
+__device__ __forceinline__ float two_to(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+
 // ---------------------------------------------------------------------------
-// Append to a cache in the rows' own type: one workgroup per token, an item a thread.
+// 4-bit groups
+// ---------------------------------------------------------------------------
+template <typename T> struct GroupRange;                     // exponents of a group of numbers of type T (owl.h)
+template <> struct GroupRange<__bf16> { static constexpr int least = -125, most = 125; };
+template <> struct GroupRange<_Float16> { static constexpr int least = -23, most = 13; };
+
+// The least e of the type's range with big <= 7 * 2^e = 1.75 * 2^(e + 2), for the bits of a finite big >= 0.
+template <typename T>
+__device__ __forceinline__ int group_exponent(uint32_t bits)
+{
+    const int e = (int)(bits >> 23) - 127 - 2 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return min(max(e, GroupRange<T>::least), GroupRange<T>::most);
+}
+
+// Greatest magnitude of a piece, as bits; infinity and what is no number lie above all others.
+template <typename T>
+__device__ __forceinline__ uint32_t greatest_bits(const Piece<T> &p)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < Piece<T>::E; ++e) m = max(m, __builtin_bit_cast(uint32_t, p.v[e]) & 0x7FFFFFFFu);
+    return m;
+}
+
+// Greatest of n = 4 or 8 neighbouring lanes' numbers, all of them active.
+template <int n>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false));
+    if constexpr (n > 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, false));
+    return v;
+}
+
+// Eight numbers of a group with exponent e as codes, nearest even, the first in the lowest four bits; beyond 6 * 2^e they are 6 * 2^e.
+__device__ __forceinline__ uint32_t codes8(const float *v, int e)
+{
+    const float s = two_to(e);
+    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+}
+
+// An item of a row on its way into a cache of 4-bit groups: `row` and `scales` are where the row's codes and scale bytes go.  A piece
+// lies in one group, a group's pieces in neighbouring lanes; D / 16 lanes that hold the same row call this together.
+template <typename T, int D>
+__device__ __forceinline__ void store_groups(const Piece<T> &a, const Piece<T> &b, int2 at, unsigned char *row, uint8_t *scales)
+{
+    constexpr int kGroups = D / 32;
+    const int ga = at.x / 32, gb = at.y / 32;
+    const uint32_t own_a = greatest_bits(a), own_b = greatest_bits(b);
+    uint32_t big_a = 0, big_b = 0;
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+        const uint32_t m = lanes_max<D / 16>(max(ga == k ? own_a : 0u, gb == k ? own_b : 0u));
+        if (ga == k) big_a = m;
+        if (gb == k) big_b = m;
+    }
+    const bool none_a = big_a >= 0x7F800000u, none_b = big_b >= 0x7F800000u;         // infinity or no number among them: no numbers
+    const int ea = group_exponent<T>(big_a), eb = group_exponent<T>(big_b);
+    *reinterpret_cast<uint32_t *>(row + at.x / 2) = none_a ? 0u : codes8(a.v, ea);
+    *reinterpret_cast<uint32_t *>(row + at.y / 2) = none_b ? 0u : codes8(b.v, eb);
+    if (at.x % 32 == 0) scales[ga] = none_a ? 255 : (uint8_t)(ea + 127);
+    if (at.y % 32 == 0) scales[gb] = none_b ? 255 : (uint8_t)(eb + 127);
+}
+
+// ---------------------------------------------------------------------------
+// Append to a cache in the rows' own type, or (kFour) of 4-bit groups, which ask nothing of other tokens either: one workgroup per
+// token, an item a thread.  kNorm: with the norms of the heads.
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 
-template <typename T, int D, bool kPairs>
+template <typename T, int D, bool kPairs, bool kNorm, bool kFour>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs p)
 {
     constexpr int E = Piece<T>::E, kItems = D / (2 * E), ES = sizeof(T);
     __shared__ double2 s_cs[D / 2];                          // [e][item]
+    __shared__ float s_gain[kNorm ? 2 * D : 1];
     fetch_args<void(AppendArgs)>();
     const int i = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int n_b = load_n_draft(p.n_new_seq, b, p.n, tid == 0 ? p.status : nullptr);
@@ -186,6 +334,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
         const int t = p.pos_ids ? p.pos_ids[token] : at;
         s_cs[tid % E * turned + tid / E] = cos_sin((double)t * (double)p.inv_freq[tid], (double)p.rot_scale);
     }
+    if constexpr (kNorm) take_gains<D, kAppendThreads>(p, s_gain);
     __syncthreads();
     const int q_heads = p.q ? p.Hq : 0, heads = q_heads + 2 * p.Hkv;
     const int64_t row = (int64_t)page * p.stride_page + at % kPage * p.stride_token;
@@ -206,13 +355,29 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
             to = p.v_cache + row + (head - q_heads - p.Hkv) * p.stride_head;
             rotate = false;
         }
-        if (head >= q_heads && page < 0) continue;
+        if (head >= q_heads && page < 0) continue;           // (the same for all items of a head)
         uint4 x = load16(from + c.x * ES), y = load16(from + c.y * ES);
-        if (rotate) {
+        if constexpr (kNorm) {
+            if (head < q_heads + p.Hkv) {
+                Piece<T> a = unpack<T>(x), z = unpack<T>(y);
+                normalise<T, kPairs, kItems>(a, z, s_gain + (head < q_heads ? 0 : D), c, (double)p.eps, rotate, s_cs + item, turned);
+                x = pack<T>(a);
+                y = pack<T>(z);
+            }
+        } else if (rotate) {
             Piece<T> a = unpack<T>(x), z = unpack<T>(y);
             turn<T, kPairs>(a, z, s_cs + item, turned);
             x = pack<T>(a);
             y = pack<T>(z);
+        }
+        if constexpr (kFour) {
+            if (head >= q_heads) {
+                const bool is_v = head >= q_heads + p.Hkv;
+                const int h = head - q_heads - (is_v ? p.Hkv : 0);
+                uint8_t *scales = (is_v ? p.v_scale : p.k_scale) + (((int64_t)page * p.Hkv + h) * kPage + at % kPage) * (D / 32);
+                store_groups<T, D>(unpack<T>(x), unpack<T>(y), c, to, scales);       // what a 16-bit cache would hold
+                continue;
+            }
         }
         store16(to + c.x * ES, x);
         store16(to + c.y * ES, y);
@@ -246,8 +411,6 @@ __device__ __forceinline__ int block_exponent(uint32_t bits)
 {
     return max((int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0), BlockRange<T>::least);
 }
-
-__device__ __forceinline__ float two_to(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
 // Four numbers, times a power of two, as e4m3 (nearest even) in one word; the block's exponent keeps them within 448.
 __device__ __forceinline__ uint32_t narrow4(const float *v, float scale)
@@ -285,11 +448,12 @@ __device__ __forceinline__ uint32_t greatest(const float *v)
 // 512 threads, with which chunks take 87.7).  By counters a wavefront waits for 60 % of its cycles there and issues for 33 %, 730 vector
 // instructions of it, most of them in 64 bits.
 // ---------------------------------------------------------------------------
-template <typename T, int D, bool kPairs>
+template <typename T, int D, bool kPairs, bool kNorm>
 __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const AppendArgs p)
 {
     constexpr int E = 8, kItems = D / (2 * E), ES = 2;
     __shared__ double2 s_cs[kPage * (D / 2 + 8)];            // [token][e][item], a token's 128 bytes further than they need
+    __shared__ float s_gain[kNorm ? 2 * D : 1];
     __shared__ uint32_t s_big[2];
     fetch_args<void(AppendArgs)>();
     const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
@@ -302,6 +466,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     const int page = good ? append_page(p, b, block, teller) : -1;
     const int half = p.rot_dim / 2, turned = p.rot_dim / (2 * E);
     if (tid < 2) s_big[tid] = 0;
+    if constexpr (kNorm) take_gains<D, kAppendThreads>(p, s_gain);
     // a thread a frequency, of every fourth (eighth) token: the chains of its angles run side by side
     constexpr int kAtOnce = kAppendThreads / (D / 2), kAngles = kPage / kAtOnce;
     const int f = tid % (D / 2);
@@ -362,9 +527,11 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
         if (r.slot < 0) return;
         const int2 at = item_at<E, kPairs>(r.item, p.rot_dim);
         uint4 u = r.x, w = r.y;
-        if (r.item < turned) {
+        if (kNorm || r.item < turned) {
             Piece<T> a = unpack<T>(u), z = unpack<T>(w);
-            turn<T, kPairs>(a, z, s_cs + r.slot * (D / 2 + 8) + r.item, turned);
+            const double2 *cs = s_cs + r.slot * (D / 2 + 8) + r.item;
+            if constexpr (kNorm) normalise<T, kPairs, kItems>(a, z, s_gain, at, (double)p.eps, r.item < turned, cs, turned);
+            else turn<T, kPairs>(a, z, cs, turned);
             u = pack<T>(a);
             w = pack<T>(z);
         }
@@ -380,8 +547,10 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     float v[2 * E] = {};
     if (mine && i >= 0) {
         Piece<T> a = unpack<T>(x), z = unpack<T>(y);
-        if (tensor == 0 && item < turned) {
-            turn<T, kPairs>(a, z, s_cs + slot * (D / 2 + 8) + item, turned);
+        if (tensor == 0 && (kNorm || item < turned)) {
+            const double2 *cs = s_cs + slot * (D / 2 + 8) + item;
+            if constexpr (kNorm) normalise<T, kPairs, kItems>(a, z, s_gain + D, c, (double)p.eps, item < turned, cs, turned);
+            else turn<T, kPairs>(a, z, cs, turned);
             a = unpack<T>(pack<T>(a));                       // what a 16-bit cache would hold
             z = unpack<T>(pack<T>(z));
         }
@@ -416,35 +585,43 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     }
 }
 
-template <typename T, int D>
-static hipError_t launch_append_as(const AppendArgs &p, int B, bool pairs, bool quant, hipStream_t s)
+template <typename T, int D, bool kPairs, bool kNorm>
+static void launch_append_rows(const AppendArgs &p, int B, Cached cached, hipStream_t s)
 {
     if constexpr (!std::is_same<T, float>::value) {
-        if (quant) {
+        if (cached == Cached::kBlocks8) {
             // blocks from the one that holds the context's end to the one that holds the last new token, wherever it begins
             const dim3 grid((p.n + 2 * kPage - 2) / kPage, p.Hkv, B);
-            if (pairs) hipLaunchKernelGGL((append_quant_kernel<T, D, true>), grid, dim3(kAppendThreads), 0, s, p);
-            else hipLaunchKernelGGL((append_quant_kernel<T, D, false>), grid, dim3(kAppendThreads), 0, s, p);
-            return hipGetLastError();
+            hipLaunchKernelGGL((append_quant_kernel<T, D, kPairs, kNorm>), grid, dim3(kAppendThreads), 0, s, p);
+            return;
+        }
+        if (cached == Cached::kGroups4) {
+            hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, true>), dim3(p.n, B), dim3(kAppendThreads), 0, s, p);
+            return;
         }
     }
-    const dim3 grid(p.n, B);
-    if (pairs) hipLaunchKernelGGL((append_kernel<T, D, true>), grid, dim3(kAppendThreads), 0, s, p);
-    else hipLaunchKernelGGL((append_kernel<T, D, false>), grid, dim3(kAppendThreads), 0, s, p);
+    hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, false>), dim3(p.n, B), dim3(kAppendThreads), 0, s, p);
+}
+
+template <typename T, int D>
+static hipError_t launch_append_as(const AppendArgs &p, int B, bool pairs, bool norm, Cached cached, hipStream_t s)
+{
+    if (pairs) norm ? launch_append_rows<T, D, true, true>(p, B, cached, s) : launch_append_rows<T, D, true, false>(p, B, cached, s);
+    else norm ? launch_append_rows<T, D, false, true>(p, B, cached, s) : launch_append_rows<T, D, false, false>(p, B, cached, s);
     return hipGetLastError();
 }
 
-int64_t append_threads(int64_t n_tokens, bool quant)
+int64_t append_threads(int64_t n_tokens, Cached cached)
 {
-    return (quant ? (n_tokens + 2 * kPage - 2) / kPage : n_tokens) * kAppendThreads;
+    return (cached == Cached::kBlocks8 ? (n_tokens + 2 * kPage - 2) / kPage : n_tokens) * kAppendThreads;
 }
 
-hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const void *q, const void *k_new, const void *v_new,
-                         const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
+hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const owl_norm_desc *norm, Cached cached, const void *q,
+                         const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
                          uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,
                          const int32_t *n_new_seq, uint32_t *status, hipStream_t s)
 {
-    const int64_t es = d.qkv_dtype == OWL_F32 ? 4 : 2, cb = k_scale ? 1 : es;
+    const int64_t es = d.qkv_dtype == OWL_F32 ? 4 : 2, cb = cached == Cached::kOwnType ? es : 1;
     AppendArgs p;
     p.q = static_cast<const unsigned char *>(q);
     p.k = static_cast<const unsigned char *>(k_new);
@@ -474,12 +651,15 @@ hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, con
     p.max_pages = d.max_pages_per_seq;
     p.max_ctx_len = d.max_ctx_len;
     p.rot_scale = a.rot_scale;
-    const bool pairs = a.rot_style == OWL_ROT_PAIRS, quant = k_scale != nullptr;
+    p.eps = norm ? norm->eps : 0.f;
+    p.q_gain = q_gain;
+    p.k_gain = k_gain;
+    const bool pairs = a.rot_style == OWL_ROT_PAIRS, normed = norm != nullptr;
     const bool wide = d.head_dim == 128;
     switch (d.qkv_dtype) {
-    case OWL_BF16: return wide ? launch_append_as<__bf16, 128>(p, d.batch, pairs, quant, s) : launch_append_as<__bf16, 64>(p, d.batch, pairs, quant, s);
-    case OWL_F16: return wide ? launch_append_as<_Float16, 128>(p, d.batch, pairs, quant, s) : launch_append_as<_Float16, 64>(p, d.batch, pairs, quant, s);
-    default: return wide ? launch_append_as<float, 128>(p, d.batch, pairs, false, s) : launch_append_as<float, 64>(p, d.batch, pairs, false, s);
+    case OWL_BF16: return wide ? launch_append_as<__bf16, 128>(p, d.batch, pairs, normed, cached, s) : launch_append_as<__bf16, 64>(p, d.batch, pairs, normed, cached, s);
+    case OWL_F16: return wide ? launch_append_as<_Float16, 128>(p, d.batch, pairs, normed, cached, s) : launch_append_as<_Float16, 64>(p, d.batch, pairs, normed, cached, s);
+    default: return wide ? launch_append_as<float, 128>(p, d.batch, pairs, normed, cached, s) : launch_append_as<float, 64>(p, d.batch, pairs, normed, cached, s);
     }
 }
 

@@ -10,6 +10,9 @@
 
 namespace owl {
 
+// How a cache holds its rows: in qkv_dtype, as 8-bit blocks, as 4-bit groups.
+enum class Cached { kOwnType, kBlocks8, kGroups4 };
+
 constexpr int kRowTile = 16;              // query rows per MFMA tile
 constexpr int kMaxSplitTokens = 16384;    // largest split of a plan with equal splits
 
@@ -97,16 +100,21 @@ hipError_t launch_commit(const owl_verify_desc &d, void *k_cache, void *v_cache,
                          const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
                          int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
 // Threads along the first dimension of the greatest grid of a call.
-int64_t append_threads(int64_t n_tokens, bool quant);
+int64_t append_threads(int64_t n_tokens, Cached cached);
 int64_t logprob_threads(const owl_logprob_desc &d, int n_cus);
-// Caches of 8-bit blocks: k_scale is null for a cache in qkv_dtype.
-hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const void *q, const void *k_new, const void *v_new,
-                         const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
+// norm: null = none.  The scales are null for a cache in qkv_dtype.
+hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const owl_norm_desc *norm, Cached cached, const void *q,
+                         const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
                          uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,
                          const int32_t *n_new_seq, uint32_t *status, hipStream_t s);
 hipError_t launch_commit_quant(const owl_verify_desc &d, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted,
                                const int32_t *n_accept, int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
+hipError_t launch_commit_groups(const owl_verify_desc &d, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
+                                const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted,
+                                const int32_t *n_accept, int32_t *new_ctx_lens, uint32_t *status, hipStream_t s);
+hipError_t launch_gather_groups(const owl_verify_desc &d, const void *cache, const uint8_t *scale, const int32_t *page_table, int seq,
+                                int64_t first, int64_t n, void *dst, uint32_t *status, hipStream_t s);
 size_t logprob_scratch_bytes(const owl_logprob_desc &d, int n_cus);
 hipError_t launch_logprobs(const owl_logprob_desc &d, const void *logits, const int32_t *tokens, float *logprob, float *entropy,
                            int32_t *top_ids, float *top_logprobs, void *scratch, uint32_t *status, int n_cus, hipStream_t s);

@@ -1,0 +1,114 @@
+"""Refusals of the calls over caches of 4-bit groups and of the append with norms: what the host can see is refused before anything is
+launched (no GPU)."""
+import ctypes
+
+import pytest
+
+from paper_2510_07535_amd import binding as B
+from test_abi_rows import A, _append_desc, _desc
+
+NORM = B.NormDesc(eps=1e-6)
+
+
+def _desc4(**over):
+    kw = dict(kv_stride_page=2 * 16 * 64, kv_stride_head=16 * 64, kv_stride_token=64)
+    kw.update(over)
+    return _desc(**kw)
+
+
+def _call(fn, desc, app, norm=NORM, **over):
+    p = dict(q=A, k_new=A, v_new=A, q_gain=A, k_gain=A, inv_freq=A, pos=0, q_out=2 * A, k_cache=A, v_cache=A, k_scale=A, v_scale=A, table=A, lens=A, n_new=0)
+    p.update(over)
+    return getattr(B.lib(), fn)(ctypes.byref(desc), None if app is None else ctypes.byref(app), None if norm is None else ctypes.byref(norm),
+                                *[p[x] for x in ("q", "k_new", "v_new", "q_gain", "k_gain", "inv_freq", "pos", "q_out", "k_cache", "v_cache", "k_scale",
+                                                 "v_scale", "table", "lens", "n_new")], 0, 0)
+
+
+FORMS = [("owl_append_kv_norm", _desc, dict(k_scale=0, v_scale=0)), ("owl_append_kv_norm", _desc, {}), ("owl_append_kv_groups", _desc4, {})]
+
+
+@pytest.mark.parametrize("fn,desc,scales", FORMS)
+@pytest.mark.parametrize("over,code", [
+    (dict(n_tokens=0), B.OWL_ERR_INVALID_ARG), (dict(n_tokens=200), B.OWL_ERR_INVALID_ARG), (dict(rot_dim=-16), B.OWL_ERR_UNSUPPORTED),
+    (dict(rot_dim=24), B.OWL_ERR_UNSUPPORTED), (dict(rot_dim=144), B.OWL_ERR_UNSUPPORTED), (dict(rot_style=2), B.OWL_ERR_UNSUPPORTED),
+    (dict(rot_scale=float("nan")), B.OWL_ERR_INVALID_ARG), (dict(q_stride=1016), B.OWL_ERR_INVALID_ARG), (dict(k_stride=248), B.OWL_ERR_INVALID_ARG),
+    (dict(v_stride=260), B.OWL_ERR_INVALID_ARG),
+])
+def test_append_refuses_shapes(fn, desc, scales, over, code):
+    assert _call(fn, desc(), _append_desc(**over), **scales) == code
+
+
+@pytest.mark.parametrize("fn,desc,scales", FORMS)
+@pytest.mark.parametrize("over", [
+    dict(k_new=0), dict(v_new=0), dict(inv_freq=0), dict(k_cache=0), dict(v_cache=0), dict(lens=0), dict(q=0), dict(q_out=0), dict(table=0),
+    dict(q=A + 8), dict(k_new=A + 2), dict(v_new=A + 4), dict(q_out=A + 8), dict(k_cache=A + 1), dict(v_cache=A + 8), dict(q_gain=A + 2), dict(k_gain=A + 1),
+])
+def test_append_refuses_pointers(fn, desc, scales, over):
+    assert _call(fn, desc(), _append_desc(), **{**scales, **over}) == B.OWL_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("fn,desc,scales", FORMS)
+@pytest.mark.parametrize("eps", [-1e-9, float("nan"), float("inf")])
+def test_append_refuses_eps(fn, desc, scales, eps):
+    assert _call(fn, desc(), _append_desc(), B.NormDesc(eps=eps), **scales) == B.OWL_ERR_INVALID_ARG
+
+
+def test_norms_and_scales_that_do_not_belong_together():
+    assert _call("owl_append_kv_norm", _desc(), _append_desc(), None) == B.OWL_ERR_INVALID_ARG
+    assert _call("owl_append_kv_norm", _desc(), _append_desc(), k_scale=0) == B.OWL_ERR_INVALID_ARG
+    assert _call("owl_append_kv_norm", _desc(), _append_desc(), v_scale=0) == B.OWL_ERR_INVALID_ARG
+    for over in (dict(k_scale=0), dict(v_scale=0), dict(k_scale=A + 8), dict(v_scale=A + 4)):
+        assert _call("owl_append_kv_groups", _desc4(), _append_desc(), **over) == B.OWL_ERR_INVALID_ARG
+    assert _call("owl_append_kv_groups", _desc4(), _append_desc(), None) == B.OWL_ERR_INVALID_ARG          # gains without norms
+    assert _call("owl_append_kv_groups", _desc4(), _append_desc(), None, q_gain=0) == B.OWL_ERR_INVALID_ARG
+
+
+BAD4 = [
+    (dict(qkv_dtype=B.OWL_F32), B.OWL_ERR_UNSUPPORTED), (dict(kv_stride_token=72), B.OWL_ERR_INVALID_ARG), (dict(kv_stride_token=48), B.OWL_ERR_INVALID_ARG),
+    (dict(kv_stride_head=16 * 64 + 8), B.OWL_ERR_INVALID_ARG), (dict(kv_stride_page=-16), B.OWL_ERR_INVALID_ARG), (dict(head_dim=96), B.OWL_ERR_UNSUPPORTED),
+    (dict(page_size=32), B.OWL_ERR_UNSUPPORTED), (dict(kv_stride_token=(1 << 26) + 16), B.OWL_ERR_UNSUPPORTED), (dict(n_q_heads=7), B.OWL_ERR_INVALID_ARG),
+]
+
+
+@pytest.mark.parametrize("over,code", BAD4)
+def test_descriptors(over, code):
+    d = _desc4(**over)
+    wide = _append_desc(k_stride=512, v_stride=512, q_stride=2048, rot_dim=64)
+    assert _call("owl_append_kv_groups", d, wide) == code
+    assert B.lib().owl_commit_kv_groups(ctypes.byref(d), A, A, A, A, A, A, A, A, 0, 0, 0) == code
+    assert B.lib().owl_gather_kv_groups(ctypes.byref(d), A, A, A, 0, 0, 10, A, 0, 0) == code
+
+
+def test_rows_of_half_a_byte_a_channel_are_legal_strides_here_only():
+    """64-byte rows of 128 channels: too short for the 8-bit calls."""
+    with pytest.raises(B.OwlError):
+        B.owl_verify_attn_quant_workspace_size(_desc4())
+
+
+def test_append_beyond_a_grid():
+    d = _desc4(max_pages_per_seq=1 << 27, n_pool_pages=1 << 27)
+    assert _call("owl_append_kv_groups", d, _append_desc(n_tokens=1 << 24)) == B.OWL_ERR_UNSUPPORTED
+    assert _call("owl_append_kv_groups", _desc4(batch=70000), _append_desc()) == B.OWL_ERR_UNSUPPORTED
+
+
+def test_commit_refuses():
+    call = lambda d=None, **o: B.lib().owl_commit_kv_groups(
+        ctypes.byref(d or _desc4()), *[o.get(x, A) for x in ("k", "v", "ks", "vs", "table", "lens", "accepted", "count")], o.get("new", 2 * A), 0, 0)
+    for x in ("k", "v", "ks", "vs", "lens", "accepted", "count", "table"):
+        assert call(**{x: 0}) == B.OWL_ERR_INVALID_ARG, x
+    for x in ("k", "v", "ks", "vs"):
+        assert call(**{x: A + 8}) == B.OWL_ERR_INVALID_ARG, x
+    assert call(new=A) == B.OWL_ERR_INVALID_ARG          # the lengths themselves
+    assert call(_desc4(max_pages_per_seq=62)) == B.OWL_ERR_INVALID_ARG
+    assert call(_desc4(n_draft=65)) == B.OWL_ERR_TOO_MANY_DRAFT
+    assert call(_desc4(batch=70000)) == B.OWL_ERR_UNSUPPORTED
+
+
+def test_gather_refuses():
+    call = lambda d=None, **o: B.lib().owl_gather_kv_groups(
+        ctypes.byref(d or _desc4()), o.get("cache", A), o.get("scale", A), o.get("table", A), o.get("seq", 0), o.get("first", 0), o.get("n", 10), o.get("dst", A), 0, 0)
+    for o in (dict(cache=0), dict(scale=0), dict(dst=0), dict(table=0), dict(seq=-1), dict(seq=2), dict(first=-1), dict(n=-1), dict(cache=A + 8),
+              dict(scale=A + 4), dict(dst=A + 2)):
+        assert call(**o) == B.OWL_ERR_INVALID_ARG, o
+    for o in (dict(first=(1 << 32) + 1), dict(n=(1 << 32) + 1)):
+        assert call(**o) == B.OWL_ERR_UNSUPPORTED, o
