@@ -477,6 +477,24 @@ owl_status owl_append_kv_groups(const owl_verify_desc *desc, const owl_append_de
                                 void *stream);
 
 /*
+ * owl_verify_attn over a cache of 4-bit groups; q in desc->qkv_dtype, which is OWL_BF16 or OWL_F16.  Sums are in 32 bits.  The products of
+ * queries and keys take a query as a sum of e4m3 numbers at the scale of its row, two (OWL_BF16) or three (OWL_F16) of them: exact down to 2^-9
+ * (2^-6) of the row's greatest number, and off by at most 2^-17 of that below; the keys are exact.  Weights are rounded to qkv_dtype before they meet the values.
+ * fp16 queries, and calls with few rows, leave fp32 partials whether or not OWL_FLAG_FP32_PARTIALS asks for them.  Values (V) up to 2^80 are summed without overflow.
+ * A query with a number that is infinite or none makes its row's answer no numbers, a key that is none those of the rows that see it, a value that is
+ * none those of all rows of its sequence and KV head.
+ * n_draft_seq as in owl_verify_attn_ragged, or NULL.  The workspace is that of owl_verify_attn_groups_workspace_size, 256-byte aligned.
+ * owl_verify_attn_groups_init and owl_verify_attn_groups_plan do what owl_verify_attn_init and owl_verify_attn_plan do, for this call.
+ */
+owl_status owl_verify_attn_groups(const owl_verify_desc *desc, const void *q, const void *k_cache, const void *v_cache,
+                                  const uint8_t *k_scale, const uint8_t *v_scale, const int32_t *page_table,
+                                  const int32_t *ctx_lens, const int32_t *tree_parent, const int32_t *n_draft_seq,
+                                  void *out, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream);
+owl_status owl_verify_attn_groups_workspace_size(const owl_verify_desc *desc, size_t *bytes);
+owl_status owl_verify_attn_groups_plan(const owl_verify_desc *desc, owl_plan *plan);
+owl_status owl_verify_attn_groups_init(const owl_verify_desc *desc);
+
+/*
  * owl_commit_kv in a cache of 4-bit groups: rows move with their scales, bit for bit.  All else as owl_commit_kv; page_table may be
  * NULL only if batch is 1.
  */

@@ -40,6 +40,7 @@ EXPORTS = (
     "owl_append_kv", "owl_append_kv_quant", "owl_verify_attn_quant", "owl_verify_attn_quant_workspace_size",
     "owl_verify_attn_quant_plan", "owl_verify_attn_quant_init", "owl_commit_kv_quant", "owl_token_logprobs", "owl_token_logprobs_workspace_size",
     "owl_append_kv_norm", "owl_append_kv_groups", "owl_commit_kv_groups", "owl_gather_kv_groups",
+    "owl_verify_attn_groups", "owl_verify_attn_groups_workspace_size", "owl_verify_attn_groups_plan", "owl_verify_attn_groups_init",
     "owl_status_str", "owl_version",
 )
 # ... and in include/owl_probe.h (measurement and self-test aids)
@@ -214,6 +215,14 @@ def lib() -> ctypes.CDLL:
         l.owl_append_kv_norm.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(AppendDesc), ctypes.POINTER(NormDesc)] + [vp] * 17
         l.owl_append_kv_groups.restype = ctypes.c_int
         l.owl_append_kv_groups.argtypes = l.owl_append_kv_norm.argtypes
+        l.owl_verify_attn_groups.restype = ctypes.c_int
+        l.owl_verify_attn_groups.argtypes = l.owl_verify_attn_quant.argtypes
+        l.owl_verify_attn_groups_workspace_size.restype = ctypes.c_int
+        l.owl_verify_attn_groups_workspace_size.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(ctypes.c_size_t)]
+        l.owl_verify_attn_groups_plan.restype = ctypes.c_int
+        l.owl_verify_attn_groups_plan.argtypes = [ctypes.POINTER(VerifyDesc), ctypes.POINTER(Plan)]
+        l.owl_verify_attn_groups_init.restype = ctypes.c_int
+        l.owl_verify_attn_groups_init.argtypes = [ctypes.POINTER(VerifyDesc)]
         l.owl_commit_kv_groups.restype = ctypes.c_int
         l.owl_commit_kv_groups.argtypes = [ctypes.POINTER(VerifyDesc)] + [vp] * 11
         l.owl_gather_kv_groups.restype = ctypes.c_int
@@ -578,6 +587,37 @@ def owl_append_kv_groups(desc: VerifyDesc, append: AppendDesc, norm, q, k_new, v
         None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
     if rc != OWL_OK:
         raise OwlError(rc, "owl_append_kv_groups")
+
+
+def owl_verify_attn_groups_workspace_size(desc: VerifyDesc) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().owl_verify_attn_groups_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "owl_verify_attn_groups_workspace_size")
+    return int(n.value)
+
+
+def owl_verify_attn_groups_plan(desc: VerifyDesc) -> Plan:
+    plan = Plan()
+    _check(lib().owl_verify_attn_groups_plan(ctypes.byref(desc), ctypes.byref(plan)), "owl_verify_attn_groups_plan")
+    return plan
+
+
+def owl_verify_attn_groups_init(desc: VerifyDesc) -> None:
+    _check(lib().owl_verify_attn_groups_init(ctypes.byref(desc)), "owl_verify_attn_groups_init")
+
+
+def owl_verify_attn_groups(desc: VerifyDesc, q, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, tree_parent, n_draft_seq,
+                           out, workspace, dev_status=None, stream: Optional[int] = None) -> None:
+    """owl_verify_attn over a cache of 4-bit groups: uint8 pools [..., D / 2], uint8 scales [n_pool_pages][Hkv][16][D / 32]."""
+    rc = lib().owl_verify_attn_groups(
+        ctypes.byref(desc), None if q is None else q.data_ptr(), None if k_cache is None else k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+        None if v_scale is None else v_scale.data_ptr(), None if page_table is None else page_table.data_ptr(),
+        None if ctx_lens is None else ctx_lens.data_ptr(), None if tree_parent is None else tree_parent.data_ptr(),
+        None if n_draft_seq is None else n_draft_seq.data_ptr(), None if out is None else out.data_ptr(),
+        None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+        None if dev_status is None else dev_status.data_ptr(), _stream() if stream is None else stream)
+    if rc != OWL_OK:
+        raise OwlError(rc, "owl_verify_attn_groups")
 
 
 def owl_commit_kv_groups(desc: VerifyDesc, k_cache, v_cache, k_scale, v_scale, page_table, ctx_lens, accepted, n_accept,

@@ -14,6 +14,8 @@ namespace {
 
 int elem_size(int dtype) { return dtype == OWL_F32 ? 4 : 2; }
 
+constexpr int kWavesPerGroup = 8;               // wavefronts of a split-KV workgroup
+
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Compute units of the current device; 256 (an MI355X) when no device answers,
@@ -82,9 +84,27 @@ owl_status check_quant_desc(const owl_verify_desc *d, Cached cached = Cached::kB
     return OWL_OK;
 }
 
-owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
+// The row tiles of a workgroup over 4-bit groups (owl_splitkv_groups.hip): as many as its wavefronts' registers hold, and fewer, in more row
+// groups, until the groups times the splits of cmin tokens fill three quarters of the compute units.
+void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int *tpw, int *wr, int *wk, int *rgs, int *group_tiles)
 {
-    owl_status st = quant ? check_quant_desc(d) : check_desc(d);
+    const int most = d->qkv_dtype == OWL_F16 ? 16 : 24;
+    int n = (RT + most - 1) / most;
+    const int64_t least = d->split_tokens > 0 ? (int64_t)align_up((size_t)d->split_tokens, kSplitQuantum) : cmin;
+    const int64_t splits = T <= least ? 1 : (T + least - 1) / least;
+    while ((RT + n - 1) / n > 4 && 4 * (int64_t)d->batch * d->n_kv_heads * splits * n < 3 * (int64_t)device_cus()) ++n;
+    *group_tiles = (RT + n - 1) / n;
+    *rgs = (RT + *group_tiles - 1) / *group_tiles;
+    const int tiles = *group_tiles;
+    *wr = tiles <= 4 ? 2 : tiles <= 8 || (tiles <= 12 && most > 16) ? 4 : 8;
+    *wk = kWavesPerGroup / *wr;
+    *tpw = (tiles + *wr - 1) / *wr;
+}
+
+owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, Cached cached = Cached::kOwnType)
+{
+    const bool quant = cached == Cached::kBlocks8, groups = cached == Cached::kGroups4;
+    owl_status st = cached == Cached::kOwnType ? check_desc(d) : check_quant_desc(d, cached);
     if (st != OWL_OK) return st;
     const int G = d->n_q_heads / d->n_kv_heads;
     const int R = G * d->n_draft;
@@ -117,7 +137,9 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     const bool fp16 = d->qkv_dtype == OWL_F16;
     const bool few = quant && (d->batch == 1 ? RT <= 4 || T * RT * d->n_kv_heads <= (fp16 ? 4000000 : 1100000)
                                              : RT <= (fp16 ? (d->max_ctx_len < 4096 ? 4 : 6) : (d->max_ctx_len < 16384 ? 2 : 4)));
-    if (few) {
+    if (groups) {
+        plan_groups(d, RT, T, cmin, &tpw, &wr, &wk, &rgs, &group_tiles);
+    } else if (few) {
         rgs = (RT + 1) / 2;
         group_tiles = (RT + rgs - 1) / rgs;
         tpw = group_tiles; wr = rgs > 1 ? 2 : 1; wk = 8;
@@ -191,7 +213,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
         else if (caps[li] == 8 && group_tiles >= 7 && piece >= 32 && share >= (group_tiles == 8 ? 64 : 256)) { tpw = 2; wr = 4; wk = 2; }
         else { wr = 8; wk = 1; tpw = (group_tiles + 7) / 8; }
     }
-    const Variant *v = find_variant(d->qkv_dtype, d->head_dim, tpw, wr, wk, false, quant);
+    const Variant *v = find_variant(d->qkv_dtype, d->head_dim, tpw, wr, wk, false, cached);
     if (!v) return OWL_ERR_UNSUPPORTED;
     fp->group_tiles = group_tiles;
     int64_t C;
@@ -262,7 +284,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
     // would need for a batch (the planned size for one sequence).
     // (8-bit blocks: own keys leave fp32 partials; and with fp16 queries, whose answer keeps 11 bits, fp16 partials would cost as much as
     // its own rounding: 3.4e-4 off the exact answer instead of 2.9e-4, for 2.5 % of the time)
-    fp->half_partials = d->qkv_dtype != OWL_F32 && !few && !(quant && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
+    fp->half_partials = d->qkv_dtype != OWL_F32 && !few && !(cached != Cached::kOwnType && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
     const size_t o_bytes = (size_t)d->head_dim * kRowTile * (fp->half_partials ? 2 : 4), ml_bytes = kPartMl * sizeof(float);
     auto bytes_of = [&](size_t slots, size_t unit) -> size_t { return align_up((size_t)d->n_kv_heads * slots * RT * unit, 256); };
     auto partials = [&](size_t slots) -> size_t { return bytes_of(slots, o_bytes) + bytes_of(slots, ml_bytes); };
@@ -319,11 +341,11 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, bool quant = false)
 owl_status ensure_lds_attr(const Variant *v)
 {
     static std::mutex mu;
-    static bool done[16][64] = {};
+    static bool done[16][128] = {};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return OWL_ERR_HIP;
     const int vi = variant_index(v);
-    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 64) return OWL_ERR_HIP;
+    if (dev < 0 || dev >= 16 || vi < 0 || vi >= 128) return OWL_ERR_HIP;
     std::lock_guard<std::mutex> lock(mu);
     if (!done[dev][vi]) {
         if (hipFuncSetAttribute(v->func, hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -401,7 +423,7 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
                               const int32_t *tree_parent, const int32_t *n_draft_seq, void *out,
                               void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream,
                               int32_t phases, hipEvent_t ev_start = nullptr, hipEvent_t ev_stop = nullptr,
-                              const uint8_t *k_scale = nullptr, const uint8_t *v_scale = nullptr);
+                              const uint8_t *k_scale = nullptr, const uint8_t *v_scale = nullptr, Cached cached = Cached::kOwnType);
 
 owl_status owl_verify_attn_phases(const owl_verify_desc *desc, const void *q, const void *k_cache,
                                   const void *v_cache, const int32_t *page_table,
@@ -429,12 +451,11 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
                               const int32_t *tree_parent, const int32_t *n_draft_seq, void *out,
                               void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream,
                               int32_t phases, hipEvent_t ev_start, hipEvent_t ev_stop, const uint8_t *k_scale,
-                              const uint8_t *v_scale)
+                              const uint8_t *v_scale, Cached cached)
 {
     if (phases < 1 || phases > OWL_PHASE_ALL) return OWL_ERR_INVALID_ARG;
-    const bool quant = k_scale != nullptr;           // a cache of 8-bit blocks
     FullPlan fp;
-    owl_status st = make_plan(desc, &fp, quant);
+    owl_status st = make_plan(desc, &fp, cached);
     if (st != OWL_OK) return st;
     if (!q || !k_cache || !v_cache || !ctx_lens || !tree_parent || !out) return OWL_ERR_INVALID_ARG;
     if (misaligned(q, 16) || misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(out, 16))
@@ -448,7 +469,7 @@ static owl_status verify_impl(const owl_verify_desc *desc, const void *q, const 
     // the profiling copy of the kernel, if the timeline hook is on and has room for this grid
     const Variant *variant = fp.variant;
     const TimelineHook hook = timeline_hook();
-    if (hook.buffer && !quant && fp.pub.n_workgroups <= hook.capacity) {
+    if (hook.buffer && cached == Cached::kOwnType && fp.pub.n_workgroups <= hook.capacity) {
         const Variant *tv = find_variant(variant->dtype, variant->D, variant->tpw, variant->wr, variant->wk, true);
         if (tv) variant = tv;
     }
@@ -679,14 +700,14 @@ owl_status owl_verify_attn_quant(const owl_verify_desc *desc, const void *q, con
 {
     if (!k_scale || !v_scale) return OWL_ERR_INVALID_ARG;
     return verify_impl(desc, q, k_cache, v_cache, page_table, ctx_lens, tree_parent, n_draft_seq, out, workspace,
-                       workspace_bytes, dev_status, stream, OWL_PHASE_ALL, nullptr, nullptr, k_scale, v_scale);
+                       workspace_bytes, dev_status, stream, OWL_PHASE_ALL, nullptr, nullptr, k_scale, v_scale, Cached::kBlocks8);
 }
 
 owl_status owl_verify_attn_quant_plan(const owl_verify_desc *desc, owl_plan *plan)
 {
     if (!plan) return OWL_ERR_INVALID_ARG;
     FullPlan fp;
-    const owl_status st = make_plan(desc, &fp, true);
+    const owl_status st = make_plan(desc, &fp, Cached::kBlocks8);
     if (st != OWL_OK) return st;
     *plan = fp.pub;
     return OWL_OK;
@@ -696,7 +717,7 @@ owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, siz
 {
     if (!bytes) return OWL_ERR_INVALID_ARG;
     FullPlan fp;
-    const owl_status st = make_plan(desc, &fp, true);
+    const owl_status st = make_plan(desc, &fp, Cached::kBlocks8);
     if (st != OWL_OK) return st;
     *bytes = fp.pub.workspace_bytes;
     return OWL_OK;
@@ -705,7 +726,7 @@ owl_status owl_verify_attn_quant_workspace_size(const owl_verify_desc *desc, siz
 owl_status owl_verify_attn_quant_init(const owl_verify_desc *desc)
 {
     FullPlan fp;
-    owl_status st = make_plan(desc, &fp, true);
+    owl_status st = make_plan(desc, &fp, Cached::kBlocks8);
     if (st != OWL_OK) return st;
     st = ensure_lds_attr(fp.variant);
     if (st != OWL_OK) return st;
@@ -732,6 +753,46 @@ owl_status owl_commit_kv_quant(const owl_verify_desc *desc, void *k_cache, void 
 }
 
 // ---- caches of 4-bit groups ----
+owl_status owl_verify_attn_groups(const owl_verify_desc *desc, const void *q, const void *k_cache, const void *v_cache,
+                                  const uint8_t *k_scale, const uint8_t *v_scale, const int32_t *page_table,
+                                  const int32_t *ctx_lens, const int32_t *tree_parent, const int32_t *n_draft_seq,
+                                  void *out, void *workspace, size_t workspace_bytes, uint32_t *dev_status, void *stream)
+{
+    if (!k_scale || !v_scale || misaligned(k_scale, 16) || misaligned(v_scale, 16)) return OWL_ERR_INVALID_ARG;
+    return verify_impl(desc, q, k_cache, v_cache, page_table, ctx_lens, tree_parent, n_draft_seq, out, workspace,
+                       workspace_bytes, dev_status, stream, OWL_PHASE_ALL, nullptr, nullptr, k_scale, v_scale, Cached::kGroups4);
+}
+
+owl_status owl_verify_attn_groups_plan(const owl_verify_desc *desc, owl_plan *plan)
+{
+    if (!plan) return OWL_ERR_INVALID_ARG;
+    FullPlan fp;
+    const owl_status st = make_plan(desc, &fp, Cached::kGroups4);
+    if (st != OWL_OK) return st;
+    *plan = fp.pub;
+    return OWL_OK;
+}
+
+owl_status owl_verify_attn_groups_workspace_size(const owl_verify_desc *desc, size_t *bytes)
+{
+    if (!bytes) return OWL_ERR_INVALID_ARG;
+    FullPlan fp;
+    const owl_status st = make_plan(desc, &fp, Cached::kGroups4);
+    if (st != OWL_OK) return st;
+    *bytes = fp.pub.workspace_bytes;
+    return OWL_OK;
+}
+
+owl_status owl_verify_attn_groups_init(const owl_verify_desc *desc)
+{
+    FullPlan fp;
+    owl_status st = make_plan(desc, &fp, Cached::kGroups4);
+    if (st != OWL_OK) return st;
+    st = ensure_lds_attr(fp.variant);
+    if (st != OWL_OK) return st;
+    return load_aux_kernels() == hipSuccess ? OWL_OK : OWL_ERR_HIP;
+}
+
 owl_status owl_commit_kv_groups(const owl_verify_desc *desc, void *k_cache, void *v_cache, uint8_t *k_scale, uint8_t *v_scale,
                                 const int32_t *page_table, const int32_t *ctx_lens, const int32_t *accepted, const int32_t *n_accept,
                                 int32_t *new_ctx_lens, uint32_t *dev_status, void *stream)

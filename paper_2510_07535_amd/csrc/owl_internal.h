@@ -54,7 +54,7 @@ struct KParams {
     long long *timeline;  // instantiations with the timeline hook only: 10 slots per workgroup (profiling aid)
 };
 
-// For caches of 8-bit blocks: the scale bytes, [page][KV head].
+// For caches of 8-bit blocks: the scale bytes, [page][KV head]; of 4-bit groups: [page][KV head][16][D / 32].
 struct QuantParams : KParams {
     const uint8_t *k_scale, *v_scale;
 };
@@ -65,20 +65,21 @@ struct QuantParams : KParams {
 struct Variant {
     int dtype, D, tpw, wr, wk;
     bool timeline;
-    bool quant;           // reads a cache of 8-bit blocks; `launch` then takes a QuantParams
+    Cached cached;        // what it reads; but for kOwnType `launch` takes a QuantParams
     size_t lds_bytes;
     // start / stop: optional events attached to the kernel's own dispatch (its begin and end), else null
     void (*launch)(const KParams &, dim3 grid, hipStream_t, hipEvent_t start, hipEvent_t stop);
     const void *func;     // for hipFuncSetAttribute
 };
 
-const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline = false, bool quant = false);
+const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline = false, Cached cached = Cached::kOwnType);
 struct VariantList {
     const Variant *first;
     int count;
 };
 VariantList quant_variants();      // owl_splitkv_quant.hip
 VariantList few_tile_variants();   // owl_splitkv_few.hip: caches of 8-bit blocks too; wk = 8, wr = 1 or, one of several row groups, 2
+VariantList group_variants();      // owl_splitkv_groups.hip
 int variant_index(const Variant *v);
 
 // Profiling hook state (set through the probe interface; read by the verify entry points).

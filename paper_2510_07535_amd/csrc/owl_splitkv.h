@@ -1643,7 +1643,7 @@ template <typename T, int D, int TPW, int WR, int WK, bool TL, bool kQuant>
 static Variant make_variant(int dtype)
 {
     using Params = typename std::conditional<kQuant, QuantParams, KParams>::type;
-    return Variant{dtype, D, TPW, WR, WK, TL, kQuant, Geo<T, D, TPW, WR, WK, kQuant>::LDS, &launch_variant<T, D, TPW, WR, WK, TL, kQuant>,
+    return Variant{dtype, D, TPW, WR, WK, TL, kQuant ? Cached::kBlocks8 : Cached::kOwnType, Geo<T, D, TPW, WR, WK, kQuant>::LDS, &launch_variant<T, D, TPW, WR, WK, TL, kQuant>,
                    reinterpret_cast<const void *>(&splitkv_kernel<T, D, TPW, WR, WK, TL, kQuant, Params>)};
 }
 

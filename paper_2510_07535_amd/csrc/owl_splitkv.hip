@@ -15,9 +15,12 @@ static const Variant kVariants[] = {
 };
 constexpr int kCount = sizeof kVariants / sizeof kVariants[0];
 
-const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline, bool quant)
+const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool timeline, Cached cached)
 {
-    const VariantList list = !quant ? VariantList{kVariants, kCount} : wk == kWaves ? few_tile_variants() : quant_variants();
+    const VariantList list = cached == Cached::kGroups4   ? group_variants()
+                             : cached == Cached::kOwnType ? VariantList{kVariants, kCount}
+                             : wk == kWaves               ? few_tile_variants()
+                                                          : quant_variants();
     for (int i = 0; i < list.count; ++i) {
         const Variant &v = list.first[i];
         if (v.dtype == dtype && v.D == D && v.tpw == tpw && v.wr == wr && v.wk == wk && v.timeline == timeline) return &v;
@@ -28,9 +31,10 @@ const Variant *find_variant(int dtype, int D, int tpw, int wr, int wk, bool time
 int variant_index(const Variant *v)
 {
     if (!v) return -1;
-    if (!v->quant) return static_cast<int>(v - kVariants);
-    const VariantList quant = quant_variants();
-    return static_cast<int>(v->wk == kWaves ? kCount + quant.count + (v - few_tile_variants().first) : kCount + (v - quant.first));
+    if (v->cached == Cached::kOwnType) return static_cast<int>(v - kVariants);
+    const VariantList quant = quant_variants(), few = few_tile_variants();
+    if (v->cached == Cached::kGroups4) return static_cast<int>(kCount + quant.count + few.count + (v - group_variants().first));
+    return static_cast<int>(v->wk == kWaves ? kCount + quant.count + (v - few.first) : kCount + (v - quant.first));
 }
 
 }  // namespace owl

@@ -489,7 +489,7 @@ static void launch_few_variant(const KParams &args, dim3 grid, hipStream_t s, hi
 
 // (wr: 1, the only row group, or 2, one of several)
 #define OWL_FEW_VARIANT(DT, T, D, TPW, GROUPS) \
-    Variant { DT, D, TPW, GROUPS, kWaves, false, true, QGeo<D>::LDS, &launch_few_variant<T, D, TPW, GROUPS == 1>, \
+    Variant { DT, D, TPW, GROUPS, kWaves, false, Cached::kBlocks8, QGeo<D>::LDS, &launch_few_variant<T, D, TPW, GROUPS == 1>, \
               reinterpret_cast<const void *>(&splitkv_few_kernel<T, D, TPW, GROUPS == 1>) }
 #define OWL_FEW_VARIANTS(DT, T, D) OWL_FEW_VARIANT(DT, T, D, 1, 1), OWL_FEW_VARIANT(DT, T, D, 2, 1), OWL_FEW_VARIANT(DT, T, D, 2, 2)
 

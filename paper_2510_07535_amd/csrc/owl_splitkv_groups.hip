@@ -1,0 +1,532 @@
+// Split-KV pass of the verify-step attention over a cache of 4-bit groups, for gfx950 (MI355X).
+//
+// The share of a workgroup, its pieces and their partials are those of owl_splitkv.h; the loop is another one, because the matrix pipe takes
+// 4-bit numbers with a scale for 32 of them as they lie in the cache:
+//   scores    S^T[key][row] = K . Q^T by v_mfma_scale_f32_16x16x128_f8f6f4, A = 16 keys' codes with their scale bytes: a lane holds the 32 channels
+//             of one group, 16 bytes, and its scale.  K is never widened.  B = Q as e4m3: a query is the sum of e4m3 numbers at one
+//             power of two for its row, x = hi + lo (+ lowest for fp16), hi the number rounded to four bits, lo the rest, again
+//             rounded, ...: two take bf16's eight bits, three fp16's eleven, exactly down to 2^-9 (2^-6) of the row's greatest, and to 2^-17 of
+//             that below.  One such product of 128 channels takes the pipe as long as two of 32 in 16 bits, so two are as
+//             cheap as the four that 16-bit keys need (measured on random operands: 70 and 112 instructions a us and SIMD).
+//   values    O^T += V^T . P^T stays in 16 bits: the groups' scales lie along the channels, not along the keys that are summed over.
+//             V is widened once for all rows (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact), on its
+//             way into LDS, and read from there by the transposing read, as in the 16-bit pass.
+//   softmax   Each wavefront has a reference of its own for each row, which stays until a score lies more than kRoom above it and then
+//             moves to the row's highest score.
+// A stage is 128 tokens: each of the eight wavefronts brings one page of K and one of V, 16 bytes (8 for head_dim 64) and a scale byte a lane
+// of each, through registers, a stage ahead, into one of two buffers in LDS.  One barrier a stage.  The wavefronts are WR row groups of
+// TPW tiles times WK key groups, which take the 32-token steps of a stage in turn and merge at the end of a piece.
+#include "owl_splitkv.h"
+
+namespace owl {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStage = 128;                          // tokens of a stage
+
+// How far a score may lie above its row's reference: a weight is at most 2^kRoom.  fp16 ends at 2^16.
+template <typename T> constexpr float kGroupRoom = 11.0f;
+template <> constexpr float kGroupRoom<__bf16> = 24.0f;
+
+template <int D, int TPW, int WR>
+struct GGeo {
+    static constexpr int WK = kWaves / WR, STEPS = 4 / WK;       // key groups; 32-token steps of a stage that each takes
+    static constexpr int NG = D / 32;                            // groups of a row
+    static constexpr int LB = D / 8, LW = LB / 4;                // bytes (words) of a page of one tensor that a lane brings
+    static constexpr int KROW = D / 2, VROW = 2 * D;             // bytes of a row in LDS: codes of K, widened V
+    static constexpr int K_BYTES = kStage * KROW, KS_BYTES = kPage * NG * 8, V_BYTES = kStage * VROW;
+    static constexpr int KS = K_BYTES, V = KS + KS_BYTES, BUFFER = V + V_BYTES;
+    static constexpr int NT = D / 16;                            // channel tiles of O^T
+    static constexpr int VPPR = VROW / 16, VSWM = VPPR >= 16 ? 7 : VPPR / 2 - 1;    // 16-byte pieces of a row of V: piece ^= (key & VSWM) << 1
+    static constexpr int TILE = NT * 1024 + 512;                 // a wavefront's part of a tile in the merge
+    static constexpr size_t LDS = 2 * BUFFER;
+    static_assert(WR * WK == kWaves && STEPS >= 1, "eight wavefronts share four steps");
+    static_assert(kWaves * TILE <= 2 * BUFFER, "the merge fits the buffers");
+    // Piece of a row of K (16 bytes), so that the fragment reads meet no bank twice.
+    static constexpr __host__ __device__ int k_piece(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 3) : piece ^ ((key >> 2) & 1); }
+};
+
+// Two e2m1 codes, of byte `kByte` of a word, times a power of two, as two numbers of type T.
+template <typename T, int kByte>
+__device__ __forceinline__ uint32_t widen_codes(uint32_t word, float scale)
+{
+    if constexpr (std::is_same<T, __bf16>::value) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(word, scale, kByte));
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 widen_word(uint32_t word, float scale)
+{
+    return make_uint4(widen_codes<T, 0>(word, scale), widen_codes<T, 1>(word, scale), widen_codes<T, 2>(word, scale), widen_codes<T, 3>(word, scale));
+}
+
+// max over the four lanes {l, l^16, l^32, l^48}
+__device__ __forceinline__ uint32_t quad_column_max_bits(uint32_t x)
+{
+    auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const uint32_t y = max((uint32_t)r[0], (uint32_t)r[1]);
+    auto r2 = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+    return max((uint32_t)r2[0], (uint32_t)r2[1]);
+}
+
+// A query tile as B operands of the scaled product: kParts e4m3 parts of the row's numbers over a power of two, which goes into the factor that takes
+// the row's products to the exponents of two, so that no size of q makes them overflow.  Lane (j, quad) holds row j;
+// the first half of an operand's 32 bytes are k = 16 quad .., the second k = 64 + 16 quad ...  With 64 channels the keys' codes stand at
+// k < 64 and again at k >= 64, and an operand's halves are two parts of the same channels.
+template <typename T, int D>
+struct Query {
+    static constexpr int kParts = std::is_same<T, __bf16>::value ? 2 : 3;
+    static constexpr int kOperands = D == 128 ? kParts : (kParts + 1) / 2;
+    i32x8 part[kOperands];
+    float c_log2;
+};
+
+template <typename T, int D>
+__device__ __forceinline__ Query<T, D> take_query(const unsigned char *row, int quad, bool on, float c_log2)
+{
+    using Q = Query<T, D>;
+    constexpr int kHalves = D / 64;
+    float x[kHalves][16];
+    uint32_t big = 0;
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(row + (64 * h + 16 * quad + 8 * c) * 2);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float lo, hi;
+                if constexpr (std::is_same<T, __bf16>::value) {
+                    lo = __builtin_bit_cast(float, words[k] << 16);
+                    hi = __builtin_bit_cast(float, words[k] & 0xFFFF0000u);
+                } else {
+                    const f16x2 v = __builtin_bit_cast(f16x2, words[k]);
+                    lo = (float)v[0];
+                    hi = (float)v[1];
+                }
+                x[h][8 * c + 2 * k] = on ? lo : 0.f;
+                x[h][8 * c + 2 * k + 1] = on ? hi : 0.f;
+            }
+        }
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) big = max(big, __builtin_bit_cast(uint32_t, x[h][e]) & 0x7FFFFFFFu);
+    big = quad_column_max_bits(big);
+    // The greatest becomes 128 .. 255, within e4m3's 448 however it is rounded; less where the row's factor would not be a normal number, for
+    // products of 0 or -infinity by 0 or infinity are no numbers.  A number that is infinite or none makes the row's factor none.
+    const int least = 1 - (((int)(__builtin_bit_cast(uint32_t, c_log2) >> 23) & 255) - 127);
+    const int s = max((int)min(big >> 23, 254u) - 7, max(least, 1)), up = 127 - s;
+    Q q;
+    q.c_log2 = big >= 0x7F800000u ? __builtin_nanf("") : fminf(__builtin_ldexpf(c_log2, -up), FLT_MAX);
+    int bytes[Q::kParts][kHalves][4];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            float rest[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rest[e] = __builtin_ldexpf(x[h][4 * w + e], up);
+#pragma unroll
+            for (int part = 0; part < Q::kParts; ++part) {
+                int b = __builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false);
+                b = __builtin_amdgcn_cvt_pk_fp8_f32(rest[2], rest[3], b, true);
+                bytes[part][h][w] = b;
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(b, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b, true);
+                rest[0] -= lo[0];
+                rest[1] -= lo[1];
+                rest[2] -= hi[0];
+                rest[3] -= hi[1];
+            }
+        }
+#pragma unroll
+    for (int o = 0; o < Q::kOperands; ++o)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (D == 128) {
+                q.part[o][w] = bytes[o][0][w];
+                q.part[o][4 + w] = bytes[o][kHalves - 1][w];
+            } else {
+                q.part[o][w] = bytes[2 * o][0][w];
+                q.part[o][4 + w] = 2 * o + 1 < Q::kParts ? bytes[2 * o + 1 < Q::kParts ? 2 * o + 1 : 0][0][w] : 0;
+            }
+        }
+    return q;
+}
+
+// S += 16 keys' codes . 16 rows: the keys' scale byte is byte kByte of `k_scale`.
+template <typename T, int D, int kByte>
+__device__ __forceinline__ f32x4 score(const uint4 &codes, int k_scale, const Query<T, D> &q)
+{
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    const i32x8 k = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
+#pragma unroll
+    for (int o = 0; o < Query<T, D>::kOperands; ++o)
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, 0, 127);
+    return s;
+}
+
+struct GPiece {
+    int b, L, Nb;                                    // sequence, its prefix length and number of drafts
+    int pos0, pos1;                                  // [pos0, pos1) of its L + Nb cached rows, pos0 a multiple of 64
+    size_t slot;                                     // where the partials of row tile 0 go
+};
+
+// A row tile of a piece as its partial: in fp32 as the accumulators stand, or normalised and in fp16 (kPartMl in owl_internal.h).
+template <int NT>
+__device__ __forceinline__ void store_partial(const KParams &p, size_t slot, f32x4 (&O)[NT + 1], float m, int lane)
+{
+    const int j = lane & 15, quad = lane >> 4;
+    const float l = O[NT][0];
+    float third = 1.0f;
+    if (!p.half_partials) {
+        float4 *po = static_cast<float4 *>(p.part_o) + slot * (size_t)(NT * 64);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) po[u * 64 + lane] = make_float4(O[u][0], O[u][1], O[u][2], O[u][3]);
+    } else {
+        const float inv_l = l > 0.f ? 1.0f / l : 0.f;          // a row that saw no key: all zeros
+        float big = 0.f;
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                O[u][r] *= inv_l;
+                big = fmaxf(big, fabsf(O[u][r]));
+            }
+        big = fmaxf(quad_column_max(big), FLT_MIN);  // (the inverse of a subnormal one may be infinite)
+        const float inv_s = 1.0f / big;
+        uint4 *po = static_cast<uint4 *>(p.part_o) + slot * (size_t)(NT / 2 * 64) + lane;
+#pragma unroll
+        for (int u = 0; u < NT; u += 2)
+            po[(u / 2) * 64] = make_uint4(pack2<_Float16>(O[u][0] * inv_s, O[u][1] * inv_s), pack2<_Float16>(O[u][2] * inv_s, O[u][3] * inv_s),
+                                           pack2<_Float16>(O[u + 1][0] * inv_s, O[u + 1][1] * inv_s),
+                                           pack2<_Float16>(O[u + 1][2] * inv_s, O[u + 1][3] * inv_s));
+        third = l * big;
+    }
+    if (quad == 0) {
+        float *stats = p.part_ml + slot * kPartMl + 3 * j;
+        stats[0] = m;
+        stats[1] = l;
+        stats[2] = third;
+    }
+}
+
+template <typename T, int D, int TPW, int WR>
+__device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned char *smem, int wave, int lane, int g, int rg, const GPiece &pc)
+{
+    using GEO = GGeo<D, TPW, WR>;
+    constexpr int NT = GEO::NT, NG = GEO::NG, LB = GEO::LB, LW = GEO::LW, WK = GEO::WK, STEPS = GEO::STEPS;
+    const int j = lane & 15, qd = lane >> 4;
+    const int wr = wave % WR, wk = wave / WR;
+    const int b = pc.b, L = pc.L, Nb = pc.Nb, pos0 = pc.pos0, pos1 = pc.pos1;
+    const int stages = (pos1 - pos0 + kStage - 1) / kStage;
+    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage;
+
+    // ---- transfers: this wavefront's page of a stage, a quarter of a row a lane ----
+    const int slot = lane >> 2, quarter = lane & 3, group = D == 128 ? quarter : quarter >> 1;
+    const int64_t head_off = (int64_t)g * p.stride_head;
+    auto page_of = [&](int s) -> int {               // unchecked; behind the piece's last page that one again
+        const int lp = min(pos0 / kPage + s * kWaves + wave, last_lp);
+        return p.page_table ? load_uniform(p.page_table + (int64_t)b * p.max_pages, min(lp, p.max_pages - 1)) : lp;
+    };
+    struct Held {
+        uint32_t k[LW], v[LW];
+        uint32_t ks, vs;
+    };
+    auto load = [&](int s, int page) -> Held {
+        const int raw = pos0 / kPage + s * kWaves + wave, lp = min(raw, last_lp);
+        if (page < 0 || page >= p.n_pool_pages || (p.page_table && lp >= p.max_pages)) {
+            flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
+            page = 0;
+        }
+        const int row = raw < last_lp ? slot : raw == last_lp ? min(slot, last_slot) : last_slot;     // rows past the end: the last one, masked later
+        const int64_t at = (int64_t)page * p.stride_page + head_off + (int64_t)row * p.stride_token + quarter * LB;
+        const int64_t s_at = (((int64_t)page * p.Hkv + g) * kPage + row) * NG + group;
+        Held h;
+        const uint32_t *k = reinterpret_cast<const uint32_t *>(static_cast<const unsigned char *>(p.k) + at);
+        const uint32_t *v = reinterpret_cast<const uint32_t *>(static_cast<const unsigned char *>(p.v) + at);
+        if constexpr (LW == 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(k), y = *reinterpret_cast<const uint4 *>(v);
+            h.k[0] = x.x; h.k[1] = x.y; h.k[2] = x.z; h.k[3] = x.w;
+            h.v[0] = y.x; h.v[1] = y.y; h.v[2] = y.z; h.v[3] = y.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(k), y = *reinterpret_cast<const uint2 *>(v);
+            h.k[0] = x.x; h.k[1] = x.y;
+            h.v[0] = y.x; h.v[1] = y.y;
+        }
+        h.ks = p.k_scale[s_at];
+        h.vs = p.v_scale[s_at];
+        return h;
+    };
+    // ... and into a buffer: codes of K, their scale bytes as [slot][group][page], V in 16 bits
+    const int key = wave * kPage + slot, v_turn = (key & GEO::VSWM) << 1;
+    auto put = [&](const Held &h, int buf) {
+        unsigned char *to = smem + buf * GEO::BUFFER;
+        if constexpr (LW == 4) {
+            *reinterpret_cast<uint4 *>(to + key * GEO::KROW + GEO::k_piece(key, quarter) * 16) = make_uint4(h.k[0], h.k[1], h.k[2], h.k[3]);
+        } else {
+            *reinterpret_cast<uint2 *>(to + key * GEO::KROW + GEO::k_piece(key, quarter >> 1) * 16 + (quarter & 1) * 8) = make_uint2(h.k[0], h.k[1]);
+        }
+        to[GEO::KS + (slot * NG + group) * 8 + wave] = (uint8_t)h.ks;
+        const float scale = __builtin_bit_cast(float, h.vs << 23);               // (255: the conversion gives no numbers)
+#pragma unroll
+        for (int w = 0; w < LW; ++w)
+            *reinterpret_cast<uint4 *>(to + GEO::V + key * GEO::VROW + (((quarter * LW + w) ^ v_turn) << 4)) = widen_word<T>(h.v[w], scale);
+    };
+
+    Held held = load(0, page_of(0));
+    int next_page = stages > 1 ? page_of(1) : 0;
+
+    // ---- query rows: tiles wr, wr + WR, ... of the row group ----
+    const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
+    const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * 2;
+    Query<T, D> q[TPW];
+    int irow[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        const int in_group = t * WR + wr, tg = rg * p.group_tiles + in_group;
+        const bool tile_ok = in_group < p.group_tiles && tg < p.RT;
+        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
+        irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
+        const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
+        q[t] = take_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd, irow[t] >= 0, p.c_log2);
+    }
+    const int my_tiles = max(0, (min(p.group_tiles, p.RT - rg * p.group_tiles) - wr + WR - 1) / WR);       // wave-uniform
+    uint64_t anc = 0;                                // the drafts that node `lane` sees
+    if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
+
+    f32x4 O[TPW][NT + 1];
+    float m[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        m[t] = kMInit;
+#pragma unroll
+        for (int u = 0; u <= NT; ++u) O[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // ---- one step of 32 tokens ----
+    const int v_key = 4 * qd + (j >> 2), v_swz = (v_key & GEO::VSWM) << 1;
+    const int v_lane = v_key * GEO::VROW + (j & 1) * 8;
+    auto step = [&](auto i_tag, auto na_tag, const unsigned char *buf, int step_pos, int scales) {
+        constexpr int i = decltype(i_tag)::value, NA = decltype(na_tag)::value;
+        const int first = (wk * STEPS + i) * 32;     // key of the stage
+        f32x4 S[NA > 0 ? NA : 1][2];
+        static_for<0, 2>([&](auto kt_tag) {
+            constexpr int kt = decltype(kt_tag)::value;
+            const int at = first + kt * kPage + j;
+            const uint4 codes = *reinterpret_cast<const uint4 *>(buf + at * GEO::KROW + GEO::k_piece(at, D == 128 ? qd : qd & 1) * 16);
+#pragma unroll
+            for (int t = 0; t < NA; ++t) S[t][kt] = score<T, D, (2 * i + kt) & 3>(codes, scales, q[t]);
+        });
+        uint4 pf[NA > 0 ? NA : 1];
+#pragma unroll
+        for (int t = 0; t < NA; ++t) {
+            f32x4 &s0 = S[t][0], &s1 = S[t][1];
+            if (step_pos + 32 > L) {                 // reaches drafts or the ragged end (uniform)
+                const int node = max(irow[t], 0);
+                uint64_t seen = ((uint64_t)__shfl((uint32_t)(anc >> 32), node) << 32) | __shfl((uint32_t)anc, node);
+                if (irow[t] < 0) seen = pos1 > L ? ~(uint64_t)0 >> (64 - Nb) : 0;       // a row without a node sees all of them
+                const int ahead = L - step_pos;      // prefix keys in this step (< 32), or minus the drafts before it
+                const uint32_t word = ahead >= 0 ? ((1u << ahead) - 1u) | (uint32_t)(seen << ahead)
+                                                 : (-ahead < 64 ? (uint32_t)(seen >> -ahead) : 0u);
+                const uint32_t va = word >> (4 * qd), vb = va >> 16;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s0[r] = (va >> r) & 1u ? s0[r] : -INFINITY;
+                    s1[r] = (vb >> r) & 1u ? s1[r] : -INFINITY;
+                }
+            }
+            const float c_log2 = q[t].c_log2;
+            const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+            // any lane's own keys can raise the alarm (uniform branch, rarely taken after the first step)
+            if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(tm, c_log2, -m[t]) > kGroupRoom<T>) != 0) {
+                const float sc = quad_column_max(tm) * c_log2;
+                const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
+                const float alpha = fast_exp2(m[t] - mn);
+                m[t] = mn;
+#pragma unroll
+                for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s0[r] = fast_exp2(__builtin_fmaf(s0[r], c_log2, -m[t]));
+                s1[r] = fast_exp2(__builtin_fmaf(s1[r], c_log2, -m[t]));
+            }
+            // (the matrix pipe takes 16-bit weights; the row sum adds the same rounded ones)
+            pf[t] = make_uint4(pack2<T>(s0[0], s0[1]), pack2<T>(s0[2], s0[3]), pack2<T>(s1[0], s1[1]), pack2<T>(s1[2], s1[3]));
+        }
+        const unsigned char *Vb = buf + GEO::V + first * GEO::VROW + v_lane;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const unsigned char *a = Vb + ((((2 * u) ^ v_swz) | ((j & 3) >> 1)) << 4);
+            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * GEO::VROW);
+            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+#pragma unroll
+            for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
+        }
+        const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
+#pragma unroll
+        for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
+    };
+
+    // ---- the loop: put stage s + 1, ask for stage s + 2, compute stage s ----
+    put(held, 0);
+    if (stages > 1) held = load(1, next_page);
+    next_page = stages > 2 ? page_of(2) : 0;
+    __syncthreads();
+    auto run = [&](auto na_tag) {
+        for (int s = 0; s < stages; ++s) {
+            const unsigned char *buf = smem + (s & 1) * GEO::BUFFER;
+            if (s + 1 < stages) put(held, (s + 1) & 1);
+            if (s + 2 < stages) held = load(s + 2, next_page);
+            next_page = s + 3 < stages ? page_of(s + 3) : 0;
+            if constexpr (decltype(na_tag)::value > 0) {
+                // the scale bytes of (key j, group) in the stage's eight pages; of them this key group's
+                const uint2 bytes = *reinterpret_cast<const uint2 *>(buf + GEO::KS + (j * NG + (qd & (NG - 1))) * 8);
+                int first_word = WK == 1 ? bytes.x : (wk >= WK / 2 ? bytes.y : bytes.x);
+                if (WK == 4 && (wk & 1)) first_word = (int)((uint32_t)first_word >> 16);
+                static_for<0, STEPS>([&](auto i_tag) {
+                    constexpr int i = decltype(i_tag)::value;
+                    const int step_pos = pos0 + s * kStage + (wk * STEPS + i) * 32;
+                    if (step_pos < pos1) step(i_tag, na_tag, buf, step_pos, i < 2 ? first_word : (int)bytes.y);
+                });
+            }
+            __syncthreads();
+        }
+    };
+    // (a wavefront computes the tiles it has)
+    if (my_tiles >= TPW) run(std::integral_constant<int, TPW>{});
+    else if (TPW > 1 && my_tiles == TPW - 1) run(std::integral_constant<int, (TPW > 1 ? TPW - 1 : 0)>{});
+    else if (TPW > 2 && my_tiles == TPW - 2) run(std::integral_constant<int, (TPW > 2 ? TPW - 2 : 0)>{});
+    else run(std::integral_constant<int, 0>{});
+
+    // ---- the key groups' sums meet in LDS, tile by tile, and become the piece's partial ----
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        const int in_group = t * WR + wr, tg = rg * p.group_tiles + in_group;
+        const bool ok = in_group < p.group_tiles && tg < p.RT;
+        if constexpr (WK > 1) {
+            const int finisher = t % WK;
+            if (t > 0) __syncthreads();
+            if (ok && wk != finisher) {
+                unsigned char *own = smem + wave * GEO::TILE;
+#pragma unroll
+                for (int u = 0; u < NT; ++u) reinterpret_cast<f32x4 *>(own)[u * 64 + lane] = O[t][u];
+                reinterpret_cast<float2 *>(own + NT * 1024)[lane] = make_float2(m[t], O[t][NT][0]);
+            }
+            __syncthreads();
+            if (ok && wk == finisher) {
+#pragma unroll
+                for (int k = 1; k < WK; ++k) {
+                    const unsigned char *src = smem + (wr + (finisher + k) % WK * WR) * GEO::TILE;
+                    const float2 ml = reinterpret_cast<const float2 *>(src + NT * 1024)[lane];
+                    const float mn = fmaxf(m[t], ml.x), a1 = fast_exp2(m[t] - mn), a2 = fast_exp2(ml.x - mn);
+                    m[t] = mn;
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) O[t][u] = O[t][u] * a1 + reinterpret_cast<const f32x4 *>(src)[u * 64 + lane] * a2;
+                    O[t][NT][0] = O[t][NT][0] * a1 + ml.y * a2;
+                }
+                store_partial<NT>(p, pc.slot + tg, O[t], m[t], lane);
+            }
+        } else if (ok) {
+            store_partial<NT>(p, pc.slot + tg, O[t], m[t], lane);
+        }
+    }
+}
+
+// The share of a workgroup, piece by piece: f(piece) is called for each, with a barrier between two.  Shares, row groups and slots are those of
+// the pass over 16-bit caches.
+template <typename F>
+__device__ __forceinline__ void for_each_piece(const KParams &p, F &&f)
+{
+    uint32_t n = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+    int rg = 0;
+    if (p.row_groups > 1) {                          // groups of a stream follow each other on one XCD
+        const uint32_t slot = n >> 3;
+        rg = (int)(slot % (uint32_t)p.row_groups);
+        n = ((slot / (uint32_t)p.row_groups) << 3) | (n & 7);
+    }
+    const int item = (int)(n / (uint32_t)p.Hkv), g = (int)(n % (uint32_t)p.Hkv);
+    const size_t head_slots = (size_t)g * p.n_slots;
+    int b = 0, before = 0, x, x1, slot0;
+    Deal deal = p.full;
+    SeqSize size{0, 0};
+    bool sized = false;
+    if (!p.dealt) {                                  // equal splits of C tokens, of one sequence each
+        const int c = item % (int)gridDim.y;
+        b = item / (int)gridDim.y;
+        if (b >= p.B || c >= p.max_splits) return;   // padding of the grid
+        x = c * (p.C / kSplitQuantum);
+        x1 = x + p.C / kSplitQuantum;
+        slot0 = b * p.max_splits + c - b;
+    } else {
+        if (item >= p.rule.max_workers) return;      // padding of the grid
+        if (p.B == 1) {
+            size = SeqSize{load_ctx_len(p.ctx_lens, 0, p.max_ctx_len, p.dev_status), load_n_draft(p.n_draft_seq, 0, p.N, p.dev_status)};
+            const int T1 = size.drafts == 0 ? 0 : size.len + size.drafts;
+            if (T1 != p.max_ctx_len + p.N) deal = deal_units(p, max(seq_units(p, T1), 1));
+        } else {
+            const BatchUnits u = batch_units(p);
+            if (u.total == 0) return;                // not one sequence has drafts
+            deal = deal_units(p, u.total);
+            if (item < deal.workers) find_unit(p, u, deal_begin(deal, item), &b, &before);
+            size = size_of(p, u, b);
+        }
+        sized = true;
+        if (item >= deal.workers) return;
+        x = deal_begin(deal, item);
+        x1 = deal_begin(deal, item + 1);
+        slot0 = item;
+    }
+    for (bool again = false; b < p.B; ++b) {
+        if (!sized) size = SeqSize{load_ctx_len(p.ctx_lens, b, p.max_ctx_len, p.dev_status), load_n_draft(p.n_draft_seq, b, p.N, p.dev_status)};
+        sized = false;
+        const int L = size.len, Nb = size.drafts;
+        const int T_b = Nb == 0 ? 0 : L + Nb;
+        const int s0 = x - before, s1 = min(x1 - before, stages_of(T_b));
+        if (s0 < s1) {
+            if (again) __syncthreads();              // LDS is free again
+            again = true;
+            f(g, rg, GPiece{b, L, Nb, s0 * kSplitQuantum, min(s1 * kSplitQuantum, T_b), (head_slots + slot0 + b) * p.RT});
+        }
+        before += seq_units(p, T_b);
+        if (before >= x1 || !p.dealt) break;
+        x = before;
+    }
+}
+
+template <typename T, int D, int TPW, int WR>
+__global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantParams p)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    fetch_args<void(QuantParams)>();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for_each_piece(p, [&](int g, int rg, const GPiece &pc) { run_group_piece<T, D, TPW, WR>(p, smem, wave, lane, g, rg, pc); });
+}
+
+template <typename T, int D, int TPW, int WR>
+static void launch_groups_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t start, hipEvent_t stop)
+{
+    const QuantParams &p = static_cast<const QuantParams &>(args);
+    if (start || stop)
+        hipExtLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, start, stop, 0, p);
+    else
+        hipLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, p);
+}
+
+#define OWL_GROUP_VARIANT(DT, T, D, TPW, WR)                                                                                      \
+    Variant { DT, D, TPW, WR, kWaves / WR, false, Cached::kGroups4, GGeo<D, TPW, WR>::LDS, &launch_groups_variant<T, D, TPW, WR>, \
+              reinterpret_cast<const void *>(&splitkv_groups_kernel<T, D, TPW, WR>) }
+#define OWL_GROUP_VARIANTS(DT, T, D)                                                                                      \
+    OWL_GROUP_VARIANT(DT, T, D, 1, 2), OWL_GROUP_VARIANT(DT, T, D, 2, 2), OWL_GROUP_VARIANT(DT, T, D, 2, 4), OWL_GROUP_VARIANT(DT, T, D, 2, 8)
+
+static const Variant kGroupVariants[] = {
+    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 128), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 8),
+    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 64), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 8),
+    OWL_GROUP_VARIANTS(OWL_F16, _Float16, 128), OWL_GROUP_VARIANTS(OWL_F16, _Float16, 64),
+};
+
+VariantList group_variants() { return VariantList{kGroupVariants, (int)(sizeof kGroupVariants / sizeof kGroupVariants[0])}; }
+
+}  // namespace owl

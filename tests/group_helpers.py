@@ -68,7 +68,7 @@ def group_case(name, seed, gain=None, stale_none=True, **kw):
             live[page, t % 16] = True
         if stale_none:
             scale = np.where(live[:, None, :, None], scale, 255).astype(np.uint8)
-        wide = np.where(live[:, None, :, None], values(raw, scale), 977.0)
+        wide = np.where(live[:, None, :, None], values(raw, scale), 0.0)
         layout = (lambda a: a) if head_major else (lambda a: a.swapaxes(1, 2))
         raws.append(np.ascontiguousarray(layout(raw)))
         scales.append(np.ascontiguousarray(scale))

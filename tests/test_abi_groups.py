@@ -112,3 +112,48 @@ def test_gather_refuses():
         assert call(**o) == B.OWL_ERR_INVALID_ARG, o
     for o in (dict(first=(1 << 32) + 1), dict(n=(1 << 32) + 1)):
         assert call(**o) == B.OWL_ERR_UNSUPPORTED, o
+
+
+@pytest.mark.parametrize("missing", ["q", "k", "v", "ks", "vs", "lens", "parent", "out"])
+def test_verify_refuses_missing_pointers(missing):
+    p = {x: 0 if x == missing else A for x in ("q", "k", "v", "ks", "vs", "table", "lens", "parent", "out", "ws")}
+    assert B.lib().owl_verify_attn_groups(ctypes.byref(_desc4()), p["q"], p["k"], p["v"], p["ks"], p["vs"], p["table"], p["lens"], p["parent"], 0,
+                                          p["out"], p["ws"], 1 << 30, 0, 0) == B.OWL_ERR_INVALID_ARG
+
+
+def test_verify_refuses_workspaces_tables_and_alignment():
+    d = _desc4()
+    size = B.owl_verify_attn_groups_workspace_size(d)
+    call = lambda **o: B.lib().owl_verify_attn_groups(
+        ctypes.byref(o.get("d", d)), o.get("q", A), o.get("k", A), A, o.get("ks", A), o.get("vs", A), A, A, A, 0, A, o.get("ws", A), o.get("bytes", size), 0, 0)
+    assert call(ws=0) == B.OWL_ERR_WORKSPACE and call(bytes=size - 1) == B.OWL_ERR_WORKSPACE
+    for o in (dict(ws=A + 128), dict(q=A + 8), dict(k=A + 8), dict(ks=A + 8), dict(vs=A + 4)):
+        assert call(**o) == B.OWL_ERR_INVALID_ARG, o
+    assert call(d=_desc4(max_pages_per_seq=62), bytes=1 << 30) == B.OWL_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("over,code", BAD4)
+def test_verify_refuses_descriptors(over, code):
+    d, plan = _desc4(**over), B.Plan()
+    for call in (B.owl_verify_attn_groups_workspace_size, B.owl_verify_attn_groups_init, B.owl_verify_attn_groups_plan):
+        with pytest.raises(B.OwlError) as e:
+            call(d)
+        assert e.value.code == code
+    assert B.lib().owl_verify_attn_groups_plan(ctypes.byref(_desc4()), None) == B.OWL_ERR_INVALID_ARG
+    assert B.lib().owl_verify_attn_groups_plan(None, ctypes.byref(plan)) == B.OWL_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [B.OWL_BF16, B.OWL_F16])
+@pytest.mark.parametrize("group", [1, 4, 8, 64])
+def test_every_plan_has_a_kernel_that_covers_its_rows(group, dtype, D):
+    for n in range(1, 65):
+        for batch, ctx, hkv in ((1, 0, 1), (1, 5003, 8), (1, 1 << 20, 2), (16, 65536, 8), (300, 700, 4)):
+            d = _desc4(n_draft=n, n_q_heads=group * hkv, n_kv_heads=hkv, batch=batch, max_ctx_len=ctx, max_pages_per_seq=(ctx + n + 15) // 16, qkv_dtype=dtype,
+                       head_dim=D)
+            p = B.owl_verify_attn_groups_plan(d)
+            assert p.workspace_bytes == B.owl_verify_attn_groups_workspace_size(d) > 0
+            assert p.row_tiles == (n * group + 15) // 16 and p.kernel_variant >= 59
+            per_group = -(-p.row_tiles // p.row_groups)
+            assert 1 <= p.tiles_per_wave <= 3 and per_group <= 8 * p.tiles_per_wave
+            assert p.split_tokens % 64 == 0 and p.split_tokens * p.max_splits >= ctx + n
