@@ -88,6 +88,15 @@ owl_status check_quant_desc(const owl_verify_desc *d, Cached cached = Cached::kB
 // groups, until the groups times the splits of cmin tokens fill three quarters of the compute units.
 void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int *tpw, int *wr, int *wk, int *rgs, int *group_tiles)
 {
+    if (RT <= 4) {                                   // keys of a wavefront's own
+        // us, own keys / shared stages, 8 KV heads, 64K: 1 tile 21.0 / 28.6, 3 tiles 34.2 / 36.0, 4 tiles 34.7 / 36.9 (fp16 39.9 / 40.2), 7 and 8
+        // tiles 53.4 / 48.6 and 53.8 / 49.3; 16 sequences of 8K-64K, 1 tile 125 / 192, 2 tiles 146 / 198.
+        *rgs = (RT + 1) / 2;
+        *group_tiles = *tpw = (RT + *rgs - 1) / *rgs;
+        *wr = *rgs > 1 ? 2 : 1;
+        *wk = kWavesPerGroup;
+        return;
+    }
     const int most = d->qkv_dtype == OWL_F16 ? 16 : 24;
     int n = (RT + most - 1) / most;
     const int64_t least = d->split_tokens > 0 ? (int64_t)align_up((size_t)d->split_tokens, kSplitQuantum) : cmin;
@@ -284,7 +293,7 @@ owl_status make_plan(const owl_verify_desc *d, FullPlan *fp, Cached cached = Cac
     // would need for a batch (the planned size for one sequence).
     // (8-bit blocks: own keys leave fp32 partials; and with fp16 queries, whose answer keeps 11 bits, fp16 partials would cost as much as
     // its own rounding: 3.4e-4 off the exact answer instead of 2.9e-4, for 2.5 % of the time)
-    fp->half_partials = d->qkv_dtype != OWL_F32 && !few && !(cached != Cached::kOwnType && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
+    fp->half_partials = d->qkv_dtype != OWL_F32 && wk < kWavesPerGroup && !(cached != Cached::kOwnType && d->qkv_dtype == OWL_F16) && !(d->flags & OWL_FLAG_FP32_PARTIALS);
     const size_t o_bytes = (size_t)d->head_dim * kRowTile * (fp->half_partials ? 2 : 4), ml_bytes = kPartMl * sizeof(float);
     auto bytes_of = [&](size_t slots, size_t unit) -> size_t { return align_up((size_t)d->n_kv_heads * slots * RT * unit, 256); };
     auto partials = [&](size_t slots) -> size_t { return bytes_of(slots, o_bytes) + bytes_of(slots, ml_bytes); };

@@ -435,10 +435,11 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     }
 }
 
-// The share of a workgroup, piece by piece: f(piece) is called for each, with a barrier between two.  Shares, row groups and slots are those of
-// the pass over 16-bit caches.
-template <typename F>
-__device__ __forceinline__ void for_each_piece(const KParams &p, F &&f)
+// The share of a workgroup, piece by piece: f(KV head, row group, piece) is called for each, with a barrier between two.  Shares, row groups and
+// slots are those of the pass over 16-bit caches.  Most lone sequences are as long as announced: ask(KV head, row group, sequence, first position) is
+// called before the length is known.
+template <typename A, typename F>
+__device__ __forceinline__ void for_each_piece(const KParams &p, A &&ask, F &&f)
 {
     uint32_t n = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
     int rg = 0;
@@ -460,9 +461,11 @@ __device__ __forceinline__ void for_each_piece(const KParams &p, F &&f)
         x = c * (p.C / kSplitQuantum);
         x1 = x + p.C / kSplitQuantum;
         slot0 = b * p.max_splits + c - b;
+        ask(g, rg, b, x * kSplitQuantum);
     } else {
         if (item >= p.rule.max_workers) return;      // padding of the grid
         if (p.B == 1) {
+            ask(g, rg, 0, deal_begin(deal, min(item, deal.workers - 1)) * kSplitQuantum);
             size = SeqSize{load_ctx_len(p.ctx_lens, 0, p.max_ctx_len, p.dev_status), load_n_draft(p.n_draft_seq, 0, p.N, p.dev_status)};
             const int T1 = size.drafts == 0 ? 0 : size.len + size.drafts;
             if (T1 != p.max_ctx_len + p.N) deal = deal_units(p, max(seq_units(p, T1), 1));
@@ -502,7 +505,267 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
     extern __shared__ __align__(16) unsigned char smem[];
     fetch_args<void(QuantParams)>();
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for_each_piece(p, [&](int g, int rg, const GPiece &pc) { run_group_piece<T, D, TPW, WR>(p, smem, wave, lane, g, rg, pc); });
+    for_each_piece(p, [](int, int, int, int) {}, [&](int g, int rg, const GPiece &pc) { run_group_piece<T, D, TPW, WR>(p, smem, wave, lane, g, rg, pc); });
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: a wavefront shares nothing until the end of a piece.  The 32-token chunks of a piece are dealt to the eight wavefronts in turn; a
+// wavefront takes all rows of its row group, TPW tiles, against its own chunks.  K's codes and scale bytes go from memory into the
+// registers of the scaled product as they are (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 8 KB of LDS of the
+// wavefront's own and read back transposed, in order, without a barrier.  kDepth chunks of each tensor are on their way while one is computed.
+// At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
+// ---------------------------------------------------------------------------
+template <int D>
+struct OGeo {
+    static constexpr int NT = D / 16, NG = D / 32, VROW = 2 * D, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
+    static constexpr int CHUNK = 2 * kPage, WAVE = CHUNK * VROW;
+    static constexpr int VSWM = GGeo<D, 1, 2>::VSWM, TILE = NT * 1024 + 512;
+    static constexpr size_t LDS = (size_t)kWaves * (WAVE > TILE ? WAVE : TILE);
+};
+
+struct OwnPages {
+    int pages, pos0;                                 // lane 2 i + h: page h of chunk i of this wavefront in the piece from pos0 on; unchecked
+};
+
+__device__ __forceinline__ int own_chunk_pages(const KParams &p, int b, int pos0, int wave, int lane, int first)
+{
+    const int lp = pos0 / kPage + (wave + kWaves * (first + (lane >> 1))) * 2 + (lane & 1);
+    return p.page_table ? p.page_table[(int64_t)b * p.max_pages + min(lp, p.max_pages - 1)] : lp;
+}
+
+// 16 (8) bytes; kOnce: no other row group reads them, and they are not kept.
+template <int LW, bool kOnce>
+__device__ __forceinline__ void load_words(uint32_t (&to)[LW], const unsigned char *from)
+{
+    typedef uint32_t Words __attribute__((ext_vector_type(LW)));
+    Words x;
+    if constexpr (kOnce) x = __builtin_nontemporal_load(reinterpret_cast<const Words *>(from));
+    else x = *reinterpret_cast<const Words *>(from);
+#pragma unroll
+    for (int w = 0; w < LW; ++w) to[w] = x[w];
+}
+
+template <typename T, int D, int TPW, bool kOnce, int kDepth>
+__device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned char *smem, int wave, int lane, int g, int rg, const GPiece &pc,
+                                              OwnPages ahead)
+{
+    using GEO = OGeo<D>;
+    constexpr int NT = GEO::NT, NG = GEO::NG, LW = GEO::LW, CHUNK = GEO::CHUNK;
+    const int j = lane & 15, qd = lane >> 4, slot = lane >> 2, quarter = lane & 3;
+    const int b = pc.b, L = pc.L, Nb = pc.Nb, pos0 = pc.pos0, pos1 = pc.pos1;
+    const int chunks = (pos1 - pos0 + CHUNK - 1) / CHUNK;
+    const int mine = max(0, (chunks - wave + kWaves - 1) / kWaves);
+    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage;
+    unsigned char *ring = smem + wave * GEO::WAVE;
+
+    int pages = ahead.pos0 == pos0 ? ahead.pages : own_chunk_pages(p, b, pos0, wave, lane, 0);
+    // Entries past the end of the piece become the chunk's first page, which is one of its pages; bad ones page 0.
+    auto checked = [&](int pg, int first) -> int {
+        const int chunk = first + (lane >> 1), lp = pos0 / kPage + (wave + kWaves * chunk) * 2 + (lane & 1);
+        const int other = __shfl_xor(pg, 1);
+        if ((lane & 1) && lp > last_lp) pg = other;
+        const bool bad = pg < 0 || pg >= p.n_pool_pages || (p.page_table && min(lp, last_lp) >= p.max_pages);
+        if (bad && chunk < mine) flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
+        return bad ? 0 : pg;
+    };
+    pages = checked(pages, 0);
+
+    // ---- transfers ----
+    struct Held {
+        uint32_t k[2][LW >= 4 ? LW : 4], v[2][LW], ks[2], vs[2];
+    };
+    Held held[kDepth];
+    const int64_t head_off = (int64_t)g * p.stride_head;
+    const uint32_t tok = (uint32_t)p.stride_token;
+    constexpr int kPiece = 16;                       // bytes of K a lane brings: the codes of a group
+    const uint32_t k_piece = (uint32_t)((qd & (NG - 1)) * kPiece), v_piece = (uint32_t)(quarter * LW * 4);
+    const uint32_t v_group = D == 128 ? quarter : quarter >> 1;
+    const uint32_t k_off = (uint32_t)j * tok + k_piece, v_off = (uint32_t)slot * tok + v_piece;
+    const uint32_t ks_off = (uint32_t)(j * NG + (qd & (NG - 1))), vs_off = (uint32_t)slot * NG + v_group;
+    auto load = [&](Held &h, int i) {
+        const bool ends = pos0 / kPage + (wave + kWaves * i) * 2 + 1 >= last_lp;      // the chunk holds the piece's last page: rows past it read it again
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t page = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + t);
+            const unsigned char *kb = static_cast<const unsigned char *>(p.k) + (page * p.stride_page + head_off);
+            const unsigned char *vb = static_cast<const unsigned char *>(p.v) + (page * p.stride_page + head_off);
+            const int64_t s_at = (page * p.Hkv + g) * (kPage * NG);
+            const uint8_t *ksb = p.k_scale + s_at, *vsb = p.v_scale + s_at;
+            uint32_t ko = k_off, vo = v_off, kso = ks_off, vso = vs_off;
+            if (ends) {
+                const int most = pos0 / kPage + (wave + kWaves * i) * 2 + t >= last_lp ? last_slot : kPage - 1;
+                const int kr = min(j, most), vr = min(slot, most);
+                ko = (uint32_t)kr * tok + k_piece;
+                vo = (uint32_t)vr * tok + v_piece;
+                kso = (uint32_t)(kr * NG + (qd & (NG - 1)));
+                vso = (uint32_t)vr * NG + v_group;
+            }
+            load_words<4, kOnce>(reinterpret_cast<uint32_t(&)[4]>(h.k[t]), kb + ko);
+            h.ks[t] = ksb[kso];
+            load_words<LW, kOnce>(h.v[t], vb + vo);
+            h.vs[t] = vsb[vso];
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+        if (d < mine) load(held[d], d);
+
+    // ---- query rows ----
+    const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
+    const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * 2;
+    Query<T, D> q[TPW];
+    int irow[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        const int tg = rg * p.group_tiles + t;
+        const bool tile_ok = t < p.group_tiles && tg < p.RT;
+        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
+        irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
+        const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
+        q[t] = take_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd, irow[t] >= 0, p.c_log2);
+    }
+    uint64_t anc = 0;                                // the drafts that node `lane` sees
+    if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
+
+    f32x4 O[TPW][NT + 1];
+    float m[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        m[t] = kMInit;
+#pragma unroll
+        for (int u = 0; u <= NT; ++u) O[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // ---- the loop ----
+    const int v_turn = (slot & GEO::VSWM) << 1;
+    unsigned char *const put_at = ring + slot * GEO::VROW;
+    const int v_key = 4 * qd + (j >> 2), v_swz = (v_key & GEO::VSWM) << 1;
+    const unsigned char *const take_at = ring + v_key * GEO::VROW + (j & 1) * 8;
+    auto step = [&](Held &h, int i, auto more_tag) {
+        f32x4 S[TPW][2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int t = 0; t < TPW; ++t)
+                S[t][kt] = score<T, D, 0>(make_uint4(h.k[kt][0], h.k[kt][1], h.k[kt][2], h.k[kt][3]), (int)h.ks[kt], q[t]);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const float scale = __builtin_bit_cast(float, h.vs[kt] << 23);           // (255: the conversion gives no numbers)
+#pragma unroll
+            for (int w = 0; w < LW; ++w)
+                *reinterpret_cast<uint4 *>(put_at + kt * kPage * GEO::VROW + (((quarter * LW + w) ^ v_turn) << 4)) = widen_word<T>(h.v[kt][w], scale);
+        }
+        if (decltype(more_tag)::value || i + kDepth < mine) load(h, i + kDepth);
+        const int step_pos = pos0 + (wave + kWaves * i) * CHUNK;
+        uint4 pf[TPW];
+#pragma unroll
+        for (int t = 0; t < TPW; ++t) {
+            f32x4 &s0 = S[t][0], &s1 = S[t][1];
+            if (step_pos + CHUNK > L) {              // reaches drafts or the ragged end (uniform)
+                const int node = max(irow[t], 0);
+                uint64_t seen = ((uint64_t)__shfl((uint32_t)(anc >> 32), node) << 32) | __shfl((uint32_t)anc, node);
+                if (irow[t] < 0) seen = pos1 > L ? ~(uint64_t)0 >> (64 - Nb) : 0;       // a row without a node sees all of them
+                const int before = L - step_pos;     // prefix keys in this chunk (< 32), or minus the drafts before it
+                const uint32_t word = before >= 0 ? ((1u << before) - 1u) | (uint32_t)(seen << before)
+                                                  : (-before < 64 ? (uint32_t)(seen >> -before) : 0u);
+                const uint32_t va = word >> (4 * qd), vb = va >> 16;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s0[r] = (va >> r) & 1u ? s0[r] : -INFINITY;
+                    s1[r] = (vb >> r) & 1u ? s1[r] : -INFINITY;
+                }
+            }
+            const float c_log2 = q[t].c_log2;
+            const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+            if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(tm, c_log2, -m[t]) > kGroupRoom<T>) != 0) {
+                const float sc = quad_column_max(tm) * c_log2;
+                const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
+                const float alpha = fast_exp2(m[t] - mn);
+                m[t] = mn;
+#pragma unroll
+                for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s0[r] = fast_exp2(__builtin_fmaf(s0[r], c_log2, -m[t]));
+                s1[r] = fast_exp2(__builtin_fmaf(s1[r], c_log2, -m[t]));
+            }
+            pf[t] = make_uint4(pack2<T>(s0[0], s0[1]), pack2<T>(s0[2], s0[3]), pack2<T>(s1[0], s1[1]), pack2<T>(s1[2], s1[3]));
+        }
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const unsigned char *a = take_at + ((((2 * u) ^ v_swz) | ((j & 3) >> 1)) << 4);
+            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * GEO::VROW);
+            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+#pragma unroll
+            for (int t = 0; t < TPW; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
+        }
+        const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
+#pragma unroll
+        for (int t = 0; t < TPW; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
+        // the pages of the 32 chunks behind those that are under way
+        if (((i + kDepth) & 31) == 31 && i + kDepth + 1 < mine) pages = checked(own_chunk_pages(p, b, pos0, wave, lane, i + kDepth + 1), i + kDepth + 1);
+    };
+    int i = 0;
+    for (; i + 2 * kDepth <= mine; i += kDepth)
+        static_for<0, kDepth>([&](auto d) { step(held[decltype(d)::value], i + decltype(d)::value, std::true_type{}); });
+    for (; i < mine; i += kDepth)
+        static_for<0, kDepth>([&](auto d) {
+            if (i + decltype(d)::value < mine) step(held[decltype(d)::value], i + decltype(d)::value, std::false_type{});
+        });
+
+    // ---- the wavefronts' sums meet, a tile after the other, and become the piece's partial ----
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        const int tg = rg * p.group_tiles + t;
+        if (t >= p.group_tiles || tg >= p.RT) break; // uniform
+        __syncthreads();                             // no wavefront reads its own part of LDS, or the tile before, any more
+        unsigned char *own = smem + wave * GEO::TILE;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) reinterpret_cast<f32x4 *>(own)[u * 64 + lane] = O[t][u];
+        reinterpret_cast<float2 *>(own + NT * 1024)[lane] = make_float2(m[t], O[t][NT][0]);
+        __syncthreads();
+        if (wave < NT) {                             // channel tile `wave`
+            float2 ml[kWaves];
+            float M = kMInit, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                ml[w] = reinterpret_cast<const float2 *>(smem + w * GEO::TILE + NT * 1024)[lane];
+                M = fmaxf(M, ml[w].x);
+            }
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float a = fast_exp2(ml[w].x - M);
+                l = __builtin_fmaf(ml[w].y, a, l);
+                const f32x4 x = reinterpret_cast<const f32x4 *>(smem + w * GEO::TILE)[wave * 64 + lane];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(x[r], a, sum[r]);
+            }
+            const size_t part = pc.slot + tg;
+            static_cast<float4 *>(p.part_o)[part * (size_t)(NT * 64) + wave * 64 + lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            if (wave == 0 && qd == 0) {
+                float *stats = p.part_ml + part * kPartMl + 3 * j;
+                stats[0] = M;
+                stats[1] = l;
+                stats[2] = 1.0f;
+            }
+        }
+    }
+}
+
+template <typename T, int D, int TPW, bool kOnce>
+__global__ void __launch_bounds__(kThreads) splitkv_groups_few_kernel(const QuantParams p)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    fetch_args<void(QuantParams)>();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    OwnPages ahead{0, -1};
+    for_each_piece(
+        p, [&](int, int, int b, int pos0) { ahead = OwnPages{own_chunk_pages(p, b, pos0, wave, lane, 0), pos0}; },
+        [&](int g, int rg, const GPiece &pc) {
+            run_own_piece<T, D, TPW, kOnce, 2>(p, smem, wave, lane, g, rg, pc, ahead);
+            ahead.pos0 = -1;
+        });
 }
 
 template <typename T, int D, int TPW, int WR>
@@ -515,6 +778,21 @@ static void launch_groups_variant(const KParams &args, dim3 grid, hipStream_t s,
         hipLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, p);
 }
 
+template <typename T, int D, int TPW, bool kOnce>
+static void launch_few_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t start, hipEvent_t stop)
+{
+    const QuantParams &p = static_cast<const QuantParams &>(args);
+    if (start || stop)
+        hipExtLaunchKernelGGL((splitkv_groups_few_kernel<T, D, TPW, kOnce>), grid, dim3(kThreads), OGeo<D>::LDS, s, start, stop, 0, p);
+    else
+        hipLaunchKernelGGL((splitkv_groups_few_kernel<T, D, TPW, kOnce>), grid, dim3(kThreads), OGeo<D>::LDS, s, p);
+}
+
+// (wk = 8: keys of a wavefront's own; wr: 1, the only row group, or 2, one of several)
+#define OWL_GROUP_FEW(DT, T, D, TPW, GROUPS)                                                                       \
+    Variant { DT, D, TPW, GROUPS, kWaves, false, Cached::kGroups4, OGeo<D>::LDS, &launch_few_variant<T, D, TPW, GROUPS == 1>, \
+              reinterpret_cast<const void *>(&splitkv_groups_few_kernel<T, D, TPW, GROUPS == 1>) }
+#define OWL_GROUP_FEWS(DT, T, D) OWL_GROUP_FEW(DT, T, D, 1, 1), OWL_GROUP_FEW(DT, T, D, 2, 1), OWL_GROUP_FEW(DT, T, D, 2, 2)
 #define OWL_GROUP_VARIANT(DT, T, D, TPW, WR)                                                                                      \
     Variant { DT, D, TPW, WR, kWaves / WR, false, Cached::kGroups4, GGeo<D, TPW, WR>::LDS, &launch_groups_variant<T, D, TPW, WR>, \
               reinterpret_cast<const void *>(&splitkv_groups_kernel<T, D, TPW, WR>) }
@@ -525,6 +803,7 @@ static const Variant kGroupVariants[] = {
     OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 128), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 8),
     OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 64), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 8),
     OWL_GROUP_VARIANTS(OWL_F16, _Float16, 128), OWL_GROUP_VARIANTS(OWL_F16, _Float16, 64),
+    OWL_GROUP_FEWS(OWL_BF16, __bf16, 128), OWL_GROUP_FEWS(OWL_BF16, __bf16, 64), OWL_GROUP_FEWS(OWL_F16, _Float16, 128), OWL_GROUP_FEWS(OWL_F16, _Float16, 64),
 };
 
 VariantList group_variants() { return VariantList{kGroupVariants, (int)(sizeof kGroupVariants / sizeof kGroupVariants[0])}; }
