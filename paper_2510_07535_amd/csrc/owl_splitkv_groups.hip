@@ -28,21 +28,25 @@ constexpr int kStage = 128;                          // tokens of a stage
 template <typename T> constexpr float kGroupRoom = 11.0f;
 template <> constexpr float kGroupRoom<__bf16> = 24.0f;
 
+// A row of widened V in LDS, padded so that neither the transposing reads, 32 bytes of 8 rows at a time, nor the stores meet a bank twice, and so that all
+// fragments are at fixed distances from one address.
+template <int D> constexpr int kVRow = 2 * D + 32;
+
 template <int D, int TPW, int WR>
 struct GGeo {
     static constexpr int WK = kWaves / WR, STEPS = 4 / WK;       // key groups; 32-token steps of a stage that each takes
     static constexpr int NG = D / 32;                            // groups of a row
     static constexpr int LB = D / 8, LW = LB / 4;                // bytes (words) of a page of one tensor that a lane brings
-    static constexpr int KROW = D / 2, VROW = 2 * D;             // bytes of a row in LDS: codes of K, widened V
-    static constexpr int K_BYTES = kStage * KROW, KS_BYTES = kPage * NG * 8, V_BYTES = kStage * VROW;
-    static constexpr int KS = K_BYTES, V = KS + KS_BYTES, BUFFER = V + V_BYTES;
+    static constexpr int KROW = D / 2;                           // bytes of a row of K's codes
+    static constexpr int K_BYTES = kStage * KROW, K_STAGE = K_BYTES + kPage * NG * 8;      // a stage of K: codes, then scales as [slot][group][page]
+    static constexpr int V_BYTES = kStage * kVRow<D>;
+    static constexpr int K = 2 * V_BYTES, MAIN = K + 2 * K_STAGE;        // two stages of V, then of K
     static constexpr int NT = D / 16;                            // channel tiles of O^T
-    static constexpr int VPPR = VROW / 16, VSWM = VPPR >= 16 ? 7 : VPPR / 2 - 1;    // 16-byte pieces of a row of V: piece ^= (key & VSWM) << 1
     static constexpr int TILE = NT * 1024 + 512;                 // a wavefront's part of a tile in the merge
-    static constexpr size_t LDS = 2 * BUFFER;
+    static constexpr size_t LDS = MAIN;
     static_assert(WR * WK == kWaves && STEPS >= 1, "eight wavefronts share four steps");
-    static_assert(kWaves * TILE <= 2 * BUFFER, "the merge fits the buffers");
-    // Piece of a row of K (16 bytes), so that the fragment reads meet no bank twice.
+    static_assert(kWaves * TILE <= MAIN, "the merge fits the buffers");
+    // Where a 16-byte piece of a row of K is, so that the fragment reads meet no bank twice.
     static constexpr __host__ __device__ int k_piece(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 3) : piece ^ ((key >> 2) & 1); }
 };
 
@@ -167,6 +171,21 @@ __device__ __forceinline__ f32x4 score(const uint4 &codes, int k_scale, const Qu
     return s;
 }
 
+// 4 or 2 words at an offset from a wave-uniform address; kOnce: no other row group reads them, and they are not kept (non-temporal).
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Words2 __attribute__((ext_vector_type(2)));
+template <int LW, bool kOnce>
+__device__ __forceinline__ void load_words(uint32_t (&to)[LW], const unsigned char *base, uint32_t at)
+{
+    typedef typename std::conditional<LW == 4, Words4, Words2>::type Words;
+    const Words *from = reinterpret_cast<const Words *>(base + at);
+    Words x;
+    if constexpr (kOnce) x = __builtin_nontemporal_load(from);
+    else x = *from;
+#pragma unroll
+    for (int w = 0; w < LW; ++w) to[w] = x[w];
+}
+
 struct GPiece {
     int b, L, Nb;                                    // sequence, its prefix length and number of drafts
     int pos0, pos1;                                  // [pos0, pos1) of its L + Nb cached rows, pos0 a multiple of 64
@@ -221,62 +240,51 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     const int wr = wave % WR, wk = wave / WR;
     const int b = pc.b, L = pc.L, Nb = pc.Nb, pos0 = pc.pos0, pos1 = pc.pos1;
     const int stages = (pos1 - pos0 + kStage - 1) / kStage;
-    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage;
 
     // ---- transfers: this wavefront's page of a stage, a quarter of a row a lane ----
     const int slot = lane >> 2, quarter = lane & 3, group = D == 128 ? quarter : quarter >> 1;
     const int64_t head_off = (int64_t)g * p.stride_head;
-    auto page_of = [&](int s) -> int {               // unchecked; behind the piece's last page that one again
-        const int lp = min(pos0 / kPage + s * kWaves + wave, last_lp);
-        return p.page_table ? load_uniform(p.page_table + (int64_t)b * p.max_pages, min(lp, p.max_pages - 1)) : lp;
+    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage, lp0 = pos0 / kPage + wave;
+    // Lane i holds the page of stage first + i, checked; bad ones are page 0, and behind the piece's last page that one again.
+    auto stage_pages = [&](int first) -> int {
+        const int lp = min(lp0 + (first + lane) * kWaves, last_lp);
+        int pg = lp;
+        if (p.page_table) pg = p.page_table[(int64_t)b * p.max_pages + min(lp, p.max_pages - 1)];
+        const bool bad = pg < 0 || pg >= p.n_pool_pages || (p.page_table && lp >= p.max_pages);
+        if (bad) flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
+        return bad ? 0 : pg;
     };
+    int pages = stage_pages(0);
     struct Held {
-        uint32_t k[LW], v[LW];
-        uint32_t ks, vs;
+        uint32_t k[LW], v[LW], ks, vs;
     };
-    auto load = [&](int s, int page) -> Held {
-        const int raw = pos0 / kPage + s * kWaves + wave, lp = min(raw, last_lp);
-        if (page < 0 || page >= p.n_pool_pages || (p.page_table && lp >= p.max_pages)) {
-            flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
-            page = 0;
-        }
-        const int row = raw < last_lp ? slot : raw == last_lp ? min(slot, last_slot) : last_slot;     // rows past the end: the last one, masked later
-        const int64_t at = (int64_t)page * p.stride_page + head_off + (int64_t)row * p.stride_token + quarter * LB;
-        const int64_t s_at = (((int64_t)page * p.Hkv + g) * kPage + row) * NG + group;
+    // No load is in a branch: the compiler would wait for all of them where the paths meet.
+    const uint32_t tok = (uint32_t)p.stride_token, slot_off = (uint32_t)slot * tok, slot_scale = (uint32_t)(slot * NG);
+    auto load = [&](int s) -> Held {
+        const int64_t page = __builtin_amdgcn_readlane(pages, s & 63), at = page * p.stride_page + head_off, s_at = (page * p.Hkv + g) * (kPage * NG);
+        const int most = lp0 + s * kWaves < last_lp ? kPage - 1 : last_slot;         // rows past the end: the last one again, masked later
+        const uint32_t off = min(slot_off, (uint32_t)most * tok) + quarter * LB, s_off = min(slot_scale, (uint32_t)(most * NG)) + group;
         Held h;
-        const uint32_t *k = reinterpret_cast<const uint32_t *>(static_cast<const unsigned char *>(p.k) + at);
-        const uint32_t *v = reinterpret_cast<const uint32_t *>(static_cast<const unsigned char *>(p.v) + at);
-        if constexpr (LW == 4) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(k), y = *reinterpret_cast<const uint4 *>(v);
-            h.k[0] = x.x; h.k[1] = x.y; h.k[2] = x.z; h.k[3] = x.w;
-            h.v[0] = y.x; h.v[1] = y.y; h.v[2] = y.z; h.v[3] = y.w;
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2 *>(k), y = *reinterpret_cast<const uint2 *>(v);
-            h.k[0] = x.x; h.k[1] = x.y;
-            h.v[0] = y.x; h.v[1] = y.y;
-        }
-        h.ks = p.k_scale[s_at];
-        h.vs = p.v_scale[s_at];
+        load_words<LW, false>(h.k, static_cast<const unsigned char *>(p.k) + at, off);
+        h.ks = (p.k_scale + s_at)[s_off];
+        load_words<LW, false>(h.v, static_cast<const unsigned char *>(p.v) + at, off);
+        h.vs = (p.v_scale + s_at)[s_off];
         return h;
     };
-    // ... and into a buffer: codes of K, their scale bytes as [slot][group][page], V in 16 bits
-    const int key = wave * kPage + slot, v_turn = (key & GEO::VSWM) << 1;
+    // ... and into LDS: codes of K, their scale bytes as [slot][group][page]; V in 16 bits
+    const int key = wave * kPage + slot;
+    const uint32_t k_put = GEO::K + key * GEO::KROW + (D == 128 ? GEO::k_piece(key, quarter) * 16 : GEO::k_piece(key, quarter >> 1) * 16 + (quarter & 1) * 8);
+    const uint32_t ks_put = GEO::K + GEO::K_BYTES + (slot * NG + group) * 8 + wave, v_put = key * kVRow<D> + quarter * LW * 16;
     auto put = [&](const Held &h, int buf) {
-        unsigned char *to = smem + buf * GEO::BUFFER;
-        if constexpr (LW == 4) {
-            *reinterpret_cast<uint4 *>(to + key * GEO::KROW + GEO::k_piece(key, quarter) * 16) = make_uint4(h.k[0], h.k[1], h.k[2], h.k[3]);
-        } else {
-            *reinterpret_cast<uint2 *>(to + key * GEO::KROW + GEO::k_piece(key, quarter >> 1) * 16 + (quarter & 1) * 8) = make_uint2(h.k[0], h.k[1]);
-        }
-        to[GEO::KS + (slot * NG + group) * 8 + wave] = (uint8_t)h.ks;
+        unsigned char *k_to = smem + buf * GEO::K_STAGE, *v_to = smem + (v_put + buf * GEO::V_BYTES);
+        if constexpr (LW == 4) *reinterpret_cast<uint4 *>(k_to + k_put) = make_uint4(h.k[0], h.k[1], h.k[2], h.k[3]);
+        else *reinterpret_cast<uint2 *>(k_to + k_put) = make_uint2(h.k[0], h.k[1]);
+        (k_to + ks_put)[0] = (uint8_t)h.ks;
         const float scale = __builtin_bit_cast(float, h.vs << 23);               // (255: the conversion gives no numbers)
 #pragma unroll
-        for (int w = 0; w < LW; ++w)
-            *reinterpret_cast<uint4 *>(to + GEO::V + key * GEO::VROW + (((quarter * LW + w) ^ v_turn) << 4)) = widen_word<T>(h.v[w], scale);
+        for (int w = 0; w < LW; ++w) *reinterpret_cast<uint4 *>(v_to + w * 16) = widen_word<T>(h.v[w], scale);
     };
-
-    Held held = load(0, page_of(0));
-    int next_page = stages > 1 ? page_of(1) : 0;
+    Held held = load(0);
 
     // ---- query rows: tiles wr, wr + WR, ... of the row group ----
     const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
@@ -306,90 +314,100 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     }
 
     // ---- one step of 32 tokens ----
-    const int v_key = 4 * qd + (j >> 2), v_swz = (v_key & GEO::VSWM) << 1;
-    const int v_lane = v_key * GEO::VROW + (j & 1) * 8;
-    auto step = [&](auto i_tag, auto na_tag, const unsigned char *buf, int step_pos, int scales) {
+    const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * GEO::KROW + GEO::k_piece(j, D == 128 ? qd : qd & 1) * 16;
+    const uint32_t ks_take = GEO::K + GEO::K_BYTES + (j * NG + (qd & (NG - 1))) * 8;
+    const uint32_t v_take = (wk * STEPS * 32 + 4 * qd + (j >> 2)) * kVRow<D> + (j & 3) * 8;
+    auto step = [&](auto i_tag, auto na_tag, const unsigned char *k_rows, uint2 words, const unsigned char *v_rows, int step_pos) {
         constexpr int i = decltype(i_tag)::value, NA = decltype(na_tag)::value;
-        const int first = (wk * STEPS + i) * 32;     // key of the stage
-        f32x4 S[NA > 0 ? NA : 1][2];
-        static_for<0, 2>([&](auto kt_tag) {
-            constexpr int kt = decltype(kt_tag)::value;
-            const int at = first + kt * kPage + j;
-            const uint4 codes = *reinterpret_cast<const uint4 *>(buf + at * GEO::KROW + GEO::k_piece(at, D == 128 ? qd : qd & 1) * 16);
-#pragma unroll
-            for (int t = 0; t < NA; ++t) S[t][kt] = score<T, D, (2 * i + kt) & 3>(codes, scales, q[t]);
-        });
-        uint4 pf[NA > 0 ? NA : 1];
-#pragma unroll
-        for (int t = 0; t < NA; ++t) {
-            f32x4 &s0 = S[t][0], &s1 = S[t][1];
-            if (step_pos + 32 > L) {                 // reaches drafts or the ragged end (uniform)
+        // scale bytes 2 i + kt of this key group's: of the two words all (WK 1), one (2), or half of one (4)
+        int word = WK == 1 ? (i < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
+        if (WK == 4) word = (int)((uint32_t)word >> (16 * (wk & 1)));
+        const uint4 codes0 = *reinterpret_cast<const uint4 *>(k_rows + i * 32 * GEO::KROW);
+        const uint4 codes1 = *reinterpret_cast<const uint4 *>(k_rows + (i * 32 + kPage) * GEO::KROW);
+        const bool masked = step_pos + 32 > L;       // reaches drafts or the ragged end (uniform)
+        f32x4 s0, s1, n0, n1;
+        n0 = score<T, D, (2 * i) & 3>(codes0, word, q[0]);
+        n1 = score<T, D, (2 * i + 1) & 3>(codes1, word, q[0]);
+        uint4 pf[TPW];
+        static_for<0, NA>([&](auto t_tag) {
+            constexpr int t = decltype(t_tag)::value;
+            s0 = n0;
+            s1 = n1;
+            if (masked) {
                 const int node = max(irow[t], 0);
                 uint64_t seen = ((uint64_t)__shfl((uint32_t)(anc >> 32), node) << 32) | __shfl((uint32_t)anc, node);
                 if (irow[t] < 0) seen = pos1 > L ? ~(uint64_t)0 >> (64 - Nb) : 0;       // a row without a node sees all of them
                 const int ahead = L - step_pos;      // prefix keys in this step (< 32), or minus the drafts before it
-                const uint32_t word = ahead >= 0 ? ((1u << ahead) - 1u) | (uint32_t)(seen << ahead)
+                const uint32_t bits = ahead >= 0 ? ((1u << ahead) - 1u) | (uint32_t)(seen << ahead)
                                                  : (-ahead < 64 ? (uint32_t)(seen >> -ahead) : 0u);
-                const uint32_t va = word >> (4 * qd), vb = va >> 16;
+                const uint32_t va = bits >> (4 * qd), vb = va >> 16;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s0[r] = (va >> r) & 1u ? s0[r] : -INFINITY;
                     s1[r] = (vb >> r) & 1u ? s1[r] : -INFINITY;
                 }
             }
-            const float c_log2 = q[t].c_log2;
-            const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+            float x[8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -m[t]);
+                x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -m[t]);
+            }
             // any lane's own keys can raise the alarm (uniform branch, rarely taken after the first step)
-            if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(tm, c_log2, -m[t]) > kGroupRoom<T>) != 0) {
-                const float sc = quad_column_max(tm) * c_log2;
+            const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {
+                const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+                const float sc = quad_column_max(tm) * q[t].c_log2;
                 const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
                 const float alpha = fast_exp2(m[t] - mn);
                 m[t] = mn;
 #pragma unroll
                 for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -mn);
+                    x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -mn);
+                }
+            }
+            if constexpr (t + 1 < NA) {              // the next tile's products beside this one's exponentials
+                n0 = score<T, D, (2 * i) & 3>(codes0, word, q[t + 1]);
+                n1 = score<T, D, (2 * i + 1) & 3>(codes1, word, q[t + 1]);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s0[r] = fast_exp2(__builtin_fmaf(s0[r], c_log2, -m[t]));
-                s1[r] = fast_exp2(__builtin_fmaf(s1[r], c_log2, -m[t]));
-            }
+            for (int r = 0; r < 8; ++r) x[r] = fast_exp2(x[r]);
             // (the matrix pipe takes 16-bit weights; the row sum adds the same rounded ones)
-            pf[t] = make_uint4(pack2<T>(s0[0], s0[1]), pack2<T>(s0[2], s0[3]), pack2<T>(s1[0], s1[1]), pack2<T>(s1[2], s1[3]));
-        }
-        const unsigned char *Vb = buf + GEO::V + first * GEO::VROW + v_lane;
+            pf[t] = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
+        });
+        const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const unsigned char *a = Vb + ((((2 * u) ^ v_swz) | ((j & 3) >> 1)) << 4);
-            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * GEO::VROW);
+            const unsigned char *a = v_rows + i * 32 * kVRow<D> + u * 32;
+            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * kVRow<D>);
             const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
             for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
         }
-        const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 #pragma unroll
         for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
     };
 
     // ---- the loop: put stage s + 1, ask for stage s + 2, compute stage s ----
     put(held, 0);
-    if (stages > 1) held = load(1, next_page);
-    next_page = stages > 2 ? page_of(2) : 0;
+    held = load(1);
     __syncthreads();
     auto run = [&](auto na_tag) {
         for (int s = 0; s < stages; ++s) {
-            const unsigned char *buf = smem + (s & 1) * GEO::BUFFER;
-            if (s + 1 < stages) put(held, (s + 1) & 1);
-            if (s + 2 < stages) held = load(s + 2, next_page);
-            next_page = s + 3 < stages ? page_of(s + 3) : 0;
+            const int buf = s & 1;
+            put(held, buf ^ 1);
+            if (((s + 2) & 63) == 0 && s + 2 < stages) pages = stage_pages(s + 2);
+            held = load(s + 2);
             if constexpr (decltype(na_tag)::value > 0) {
-                // the scale bytes of (key j, group) in the stage's eight pages; of them this key group's
-                const uint2 bytes = *reinterpret_cast<const uint2 *>(buf + GEO::KS + (j * NG + (qd & (NG - 1))) * 8);
-                int first_word = WK == 1 ? bytes.x : (wk >= WK / 2 ? bytes.y : bytes.x);
-                if (WK == 4 && (wk & 1)) first_word = (int)((uint32_t)first_word >> 16);
+                const unsigned char *k_rows = smem + (k_take + buf * GEO::K_STAGE), *v_rows = smem + (v_take + buf * GEO::V_BYTES);
+                const uint2 words = *reinterpret_cast<const uint2 *>(smem + (ks_take + buf * GEO::K_STAGE));
+                const int pos = pos0 + s * kStage + wk * STEPS * 32;
                 static_for<0, STEPS>([&](auto i_tag) {
                     constexpr int i = decltype(i_tag)::value;
-                    const int step_pos = pos0 + s * kStage + (wk * STEPS + i) * 32;
-                    if (step_pos < pos1) step(i_tag, na_tag, buf, step_pos, i < 2 ? first_word : (int)bytes.y);
+                    if (pos + i * 32 < pos1) step(i_tag, na_tag, k_rows, words, v_rows, pos + i * 32);       // uniform
                 });
             }
             __syncthreads();
@@ -517,9 +535,9 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
 // ---------------------------------------------------------------------------
 template <int D>
 struct OGeo {
-    static constexpr int NT = D / 16, NG = D / 32, VROW = 2 * D, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
+    static constexpr int NT = D / 16, NG = D / 32, VROW = kVRow<D>, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
     static constexpr int CHUNK = 2 * kPage, WAVE = CHUNK * VROW;
-    static constexpr int VSWM = GGeo<D, 1, 2>::VSWM, TILE = NT * 1024 + 512;
+    static constexpr int TILE = NT * 1024 + 512;
     static constexpr size_t LDS = (size_t)kWaves * (WAVE > TILE ? WAVE : TILE);
 };
 
@@ -533,18 +551,6 @@ __device__ __forceinline__ int own_chunk_pages(const KParams &p, int b, int pos0
     return p.page_table ? p.page_table[(int64_t)b * p.max_pages + min(lp, p.max_pages - 1)] : lp;
 }
 
-// 16 (8) bytes; kOnce: no other row group reads them, and they are not kept.
-template <int LW, bool kOnce>
-__device__ __forceinline__ void load_words(uint32_t (&to)[LW], const unsigned char *from)
-{
-    typedef uint32_t Words __attribute__((ext_vector_type(LW)));
-    Words x;
-    if constexpr (kOnce) x = __builtin_nontemporal_load(reinterpret_cast<const Words *>(from));
-    else x = *reinterpret_cast<const Words *>(from);
-#pragma unroll
-    for (int w = 0; w < LW; ++w) to[w] = x[w];
-}
-
 template <typename T, int D, int TPW, bool kOnce, int kDepth>
 __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned char *smem, int wave, int lane, int g, int rg, const GPiece &pc,
                                               OwnPages ahead)
@@ -555,55 +561,40 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     const int b = pc.b, L = pc.L, Nb = pc.Nb, pos0 = pc.pos0, pos1 = pc.pos1;
     const int chunks = (pos1 - pos0 + CHUNK - 1) / CHUNK;
     const int mine = max(0, (chunks - wave + kWaves - 1) / kWaves);
-    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage;
     unsigned char *ring = smem + wave * GEO::WAVE;
 
-    int pages = ahead.pos0 == pos0 ? ahead.pages : own_chunk_pages(p, b, pos0, wave, lane, 0);
-    // Entries past the end of the piece become the chunk's first page, which is one of its pages; bad ones page 0.
+    // Bad pages are page 0; behind the piece's end it is the piece's last one.
+    const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage, lp0 = pos0 / kPage + wave * 2;
     auto checked = [&](int pg, int first) -> int {
-        const int chunk = first + (lane >> 1), lp = pos0 / kPage + (wave + kWaves * chunk) * 2 + (lane & 1);
+        const int lp = lp0 + (first + (lane >> 1)) * (2 * kWaves) + (lane & 1);
         const int other = __shfl_xor(pg, 1);
-        if ((lane & 1) && lp > last_lp) pg = other;
+        if ((lane & 1) && lp > last_lp) pg = other;  // the last chunk's second page
         const bool bad = pg < 0 || pg >= p.n_pool_pages || (p.page_table && min(lp, last_lp) >= p.max_pages);
-        if (bad && chunk < mine) flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
+        if (bad && lp - (lane & 1) <= last_lp) flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
         return bad ? 0 : pg;
     };
-    pages = checked(pages, 0);
+    int pages = checked(ahead.pos0 == pos0 ? ahead.pages : own_chunk_pages(p, b, pos0, wave, lane, 0), 0);
 
     // ---- transfers ----
     struct Held {
-        uint32_t k[2][LW >= 4 ? LW : 4], v[2][LW], ks[2], vs[2];
+        uint32_t k[2][4], v[2][LW], ks[2], vs[2];
     };
     Held held[kDepth];
     const int64_t head_off = (int64_t)g * p.stride_head;
     const uint32_t tok = (uint32_t)p.stride_token;
-    constexpr int kPiece = 16;                       // bytes of K a lane brings: the codes of a group
-    const uint32_t k_piece = (uint32_t)((qd & (NG - 1)) * kPiece), v_piece = (uint32_t)(quarter * LW * 4);
-    const uint32_t v_group = D == 128 ? quarter : quarter >> 1;
-    const uint32_t k_off = (uint32_t)j * tok + k_piece, v_off = (uint32_t)slot * tok + v_piece;
-    const uint32_t ks_off = (uint32_t)(j * NG + (qd & (NG - 1))), vs_off = (uint32_t)slot * NG + v_group;
+    const uint32_t k_piece = (uint32_t)((qd & (NG - 1)) * 16), v_piece = (uint32_t)(quarter * LW * 4), ks_piece = qd & (NG - 1), vs_piece = D == 128 ? quarter : quarter >> 1;
+    const uint32_t k_slot = (uint32_t)j * tok, v_slot = (uint32_t)slot * tok, ks_slot = (uint32_t)(j * NG), vs_slot = (uint32_t)(slot * NG);
     auto load = [&](Held &h, int i) {
-        const bool ends = pos0 / kPage + (wave + kWaves * i) * 2 + 1 >= last_lp;      // the chunk holds the piece's last page: rows past it read it again
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int64_t page = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + t);
-            const unsigned char *kb = static_cast<const unsigned char *>(p.k) + (page * p.stride_page + head_off);
-            const unsigned char *vb = static_cast<const unsigned char *>(p.v) + (page * p.stride_page + head_off);
+            const int64_t page = __builtin_amdgcn_readlane(pages, (i & 31) * 2 + t), at = page * p.stride_page + head_off;
+            const int most = lp0 + i * (2 * kWaves) + t < last_lp ? kPage - 1 : last_slot;      // rows past the end: the last one again, masked later
+            const uint32_t bytes = (uint32_t)most * tok, scales = (uint32_t)(most * NG);
             const int64_t s_at = (page * p.Hkv + g) * (kPage * NG);
-            const uint8_t *ksb = p.k_scale + s_at, *vsb = p.v_scale + s_at;
-            uint32_t ko = k_off, vo = v_off, kso = ks_off, vso = vs_off;
-            if (ends) {
-                const int most = pos0 / kPage + (wave + kWaves * i) * 2 + t >= last_lp ? last_slot : kPage - 1;
-                const int kr = min(j, most), vr = min(slot, most);
-                ko = (uint32_t)kr * tok + k_piece;
-                vo = (uint32_t)vr * tok + v_piece;
-                kso = (uint32_t)(kr * NG + (qd & (NG - 1)));
-                vso = (uint32_t)vr * NG + v_group;
-            }
-            load_words<4, kOnce>(reinterpret_cast<uint32_t(&)[4]>(h.k[t]), kb + ko);
-            h.ks[t] = ksb[kso];
-            load_words<LW, kOnce>(h.v[t], vb + vo);
-            h.vs[t] = vsb[vso];
+            load_words<4, kOnce>(h.k[t], static_cast<const unsigned char *>(p.k) + at, min(k_slot, bytes) + k_piece);
+            h.ks[t] = (p.k_scale + s_at)[min(ks_slot, scales) + ks_piece];
+            load_words<LW, kOnce>(h.v[t], static_cast<const unsigned char *>(p.v) + at, min(v_slot, bytes) + v_piece);
+            h.vs[t] = (p.v_scale + s_at)[min(vs_slot, scales) + vs_piece];
         }
     };
 #pragma unroll
@@ -636,10 +627,8 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
         for (int u = 0; u <= NT; ++u) O[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // ---- the loop ----
-    const int v_turn = (slot & GEO::VSWM) << 1;
-    unsigned char *const put_at = ring + slot * GEO::VROW;
-    const int v_key = 4 * qd + (j >> 2), v_swz = (v_key & GEO::VSWM) << 1;
-    const unsigned char *const take_at = ring + v_key * GEO::VROW + (j & 1) * 8;
+    unsigned char *const put_at = ring + slot * GEO::VROW + quarter * LW * 16;
+    const unsigned char *const take_at = ring + (4 * qd + (j >> 2)) * GEO::VROW + (j & 3) * 8;
     auto step = [&](Held &h, int i, auto more_tag) {
         f32x4 S[TPW][2];
 #pragma unroll
@@ -652,7 +641,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
             const float scale = __builtin_bit_cast(float, h.vs[kt] << 23);           // (255: the conversion gives no numbers)
 #pragma unroll
             for (int w = 0; w < LW; ++w)
-                *reinterpret_cast<uint4 *>(put_at + kt * kPage * GEO::VROW + (((quarter * LW + w) ^ v_turn) << 4)) = widen_word<T>(h.v[kt][w], scale);
+                *reinterpret_cast<uint4 *>(put_at + kt * kPage * GEO::VROW + w * 16) = widen_word<T>(h.v[kt][w], scale);
         }
         if (decltype(more_tag)::value || i + kDepth < mine) load(h, i + kDepth);
         const int step_pos = pos0 + (wave + kWaves * i) * CHUNK;
@@ -674,26 +663,34 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
                     s1[r] = (vb >> r) & 1u ? s1[r] : -INFINITY;
                 }
             }
-            const float c_log2 = q[t].c_log2;
-            const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-            if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(tm, c_log2, -m[t]) > kGroupRoom<T>) != 0) {
-                const float sc = quad_column_max(tm) * c_log2;
+            float x[8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -m[t]);
+                x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -m[t]);
+            }
+            const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {
+                const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+                const float sc = quad_column_max(tm) * q[t].c_log2;
                 const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
                 const float alpha = fast_exp2(m[t] - mn);
                 m[t] = mn;
 #pragma unroll
                 for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -mn);
+                    x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -mn);
+                }
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s0[r] = fast_exp2(__builtin_fmaf(s0[r], c_log2, -m[t]));
-                s1[r] = fast_exp2(__builtin_fmaf(s1[r], c_log2, -m[t]));
-            }
-            pf[t] = make_uint4(pack2<T>(s0[0], s0[1]), pack2<T>(s0[2], s0[3]), pack2<T>(s1[0], s1[1]), pack2<T>(s1[2], s1[3]));
+            for (int r = 0; r < 8; ++r) x[r] = fast_exp2(x[r]);
+            pf[t] = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
         }
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const unsigned char *a = take_at + ((((2 * u) ^ v_swz) | ((j & 3) >> 1)) << 4);
+            const unsigned char *a = take_at + u * 32;
             const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * GEO::VROW);
             const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
