@@ -105,7 +105,7 @@ void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int 
     *group_tiles = (RT + n - 1) / n;
     *rgs = (RT + *group_tiles - 1) / *group_tiles;
     const int tiles = *group_tiles;
-    *wr = tiles <= 4 ? 2 : tiles <= 8 || (tiles <= 12 && most > 16) ? 4 : 8;
+    *wr = tiles <= 4 ? 2 : tiles <= 8 ? 4 : 8;
     *wk = kWavesPerGroup / *wr;
     *tpw = (tiles + *wr - 1) / *wr;
 }

@@ -40,7 +40,7 @@ struct GGeo {
     static constexpr int KROW = D / 2;                           // bytes of a row of K's codes
     static constexpr int K_BYTES = kStage * KROW, K_STAGE = K_BYTES + kPage * NG * 8;      // a stage of K: codes, then scales as [slot][group][page]
     static constexpr int V_BYTES = kStage * kVRow<D>;
-    static constexpr int K = 2 * V_BYTES, MAIN = K + 2 * K_STAGE;        // two stages of V, then of K
+    static constexpr int K = 2 * V_BYTES, MAIN = K + 3 * K_STAGE;        // two stages of V, then three of K
     static constexpr int NT = D / 16;                            // channel tiles of O^T
     static constexpr int TILE = NT * 1024 + 512;                 // a wavefront's part of a tile in the merge
     static constexpr size_t LDS = MAIN;
@@ -245,46 +245,62 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     const int slot = lane >> 2, quarter = lane & 3, group = D == 128 ? quarter : quarter >> 1;
     const int64_t head_off = (int64_t)g * p.stride_head;
     const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage, lp0 = pos0 / kPage + wave;
-    // Lane i holds the page of stage first + i, checked; bad ones are page 0, and behind the piece's last page that one again.
-    auto stage_pages = [&](int first) -> int {
+    // Lane i holds where the page of stage first + i lies, of this KV head, in the pools and in the scales; bad pages are page 0, and behind the
+    // piece's last page it is that one again.
+    struct Where {
+        int64_t at, scales;
+    };
+    auto stage_pages = [&](int first) -> Where {
         const int lp = min(lp0 + (first + lane) * kWaves, last_lp);
         int pg = lp;
         if (p.page_table) pg = p.page_table[(int64_t)b * p.max_pages + min(lp, p.max_pages - 1)];
         const bool bad = pg < 0 || pg >= p.n_pool_pages || (p.page_table && lp >= p.max_pages);
         if (bad) flag_status(p.dev_status, OWL_DEV_BAD_PAGE);
-        return bad ? 0 : pg;
+        const int64_t page = bad ? 0 : pg;
+        return Where{page * p.stride_page + head_off, (page * p.Hkv + g) * (kPage * NG)};
     };
-    int pages = stage_pages(0);
-    struct Held {
-        uint32_t k[LW], v[LW], ks, vs;
+    Where pages = stage_pages(0);
+    auto lane_of = [](int64_t v, int i) -> int64_t {
+        return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+    };
+    struct Held {                                    // of one tensor
+        uint32_t words[LW], scale;
     };
     // No load is in a branch: the compiler would wait for all of them where the paths meet.
     const uint32_t tok = (uint32_t)p.stride_token, slot_off = (uint32_t)slot * tok, slot_scale = (uint32_t)(slot * NG);
-    auto load = [&](int s) -> Held {
-        const int64_t page = __builtin_amdgcn_readlane(pages, s & 63), at = page * p.stride_page + head_off, s_at = (page * p.Hkv + g) * (kPage * NG);
+    auto load = [&](const void *cache, const uint8_t *scales, int s) -> Held {
         const int most = lp0 + s * kWaves < last_lp ? kPage - 1 : last_slot;         // rows past the end: the last one again, masked later
-        const uint32_t off = min(slot_off, (uint32_t)most * tok) + quarter * LB, s_off = min(slot_scale, (uint32_t)(most * NG)) + group;
         Held h;
-        load_words<LW, false>(h.k, static_cast<const unsigned char *>(p.k) + at, off);
-        h.ks = (p.k_scale + s_at)[s_off];
-        load_words<LW, false>(h.v, static_cast<const unsigned char *>(p.v) + at, off);
-        h.vs = (p.v_scale + s_at)[s_off];
+        load_words<LW, false>(h.words, static_cast<const unsigned char *>(cache) + lane_of(pages.at, s & 63), min(slot_off, (uint32_t)most * tok) + quarter * LB);
+        h.scale = (scales + lane_of(pages.scales, s & 63))[min(slot_scale, (uint32_t)(most * NG)) + group];
         return h;
     };
-    // ... and into LDS: codes of K, their scale bytes as [slot][group][page]; V in 16 bits
-    const int key = wave * kPage + slot;
+    // ... and into LDS: codes of K, their scale bytes as [slot][group][page]; V in 16 bits, whose 16-byte pieces the lanes of the upper half
+    // of a row store in another order, so that eight lanes meet no bank twice
+    const int key = wave * kPage + slot, turn = D == 128 ? quarter >> 1 : 0;
     const uint32_t k_put = GEO::K + key * GEO::KROW + (D == 128 ? GEO::k_piece(key, quarter) * 16 : GEO::k_piece(key, quarter >> 1) * 16 + (quarter & 1) * 8);
     const uint32_t ks_put = GEO::K + GEO::K_BYTES + (slot * NG + group) * 8 + wave, v_put = key * kVRow<D> + quarter * LW * 16;
-    auto put = [&](const Held &h, int buf) {
-        unsigned char *k_to = smem + buf * GEO::K_STAGE, *v_to = smem + (v_put + buf * GEO::V_BYTES);
-        if constexpr (LW == 4) *reinterpret_cast<uint4 *>(k_to + k_put) = make_uint4(h.k[0], h.k[1], h.k[2], h.k[3]);
-        else *reinterpret_cast<uint2 *>(k_to + k_put) = make_uint2(h.k[0], h.k[1]);
-        (k_to + ks_put)[0] = (uint8_t)h.ks;
-        const float scale = __builtin_bit_cast(float, h.vs << 23);               // (255: the conversion gives no numbers)
-#pragma unroll
-        for (int w = 0; w < LW; ++w) *reinterpret_cast<uint4 *>(v_to + w * 16) = widen_word<T>(h.v[w], scale);
+    auto put_k = [&](const Held &h, uint32_t ring) {
+        if constexpr (LW == 4) *reinterpret_cast<uint4 *>(smem + (k_put + ring)) = make_uint4(h.words[0], h.words[1], h.words[2], h.words[3]);
+        else *reinterpret_cast<uint2 *>(smem + (k_put + ring)) = make_uint2(h.words[0], h.words[1]);
+        smem[ks_put + ring] = (uint8_t)h.scale;
     };
-    Held held = load(0);
+    auto put_v = [&](const Held &h, int buf) {
+        const float scale = __builtin_bit_cast(float, h.scale << 23);            // (255: the conversion gives no numbers)
+        const uint32_t at = v_put + buf * GEO::V_BYTES;
+        unsigned char *even = smem + (at + turn * 16), *odd = smem + (at + 16 - turn * 16);
+#pragma unroll
+        for (int w = 0; w < LW; w += 2) {
+            const uint32_t a = turn ? h.words[w + 1] : h.words[w], c = turn ? h.words[w] : h.words[w + 1];
+            *reinterpret_cast<uint4 *>(even + w * 16) = widen_word<T>(a, scale);
+            *reinterpret_cast<uint4 *>(odd + w * 16) = widen_word<T>(c, scale);
+        }
+    };
+    // V of stage s is put while stage s - 1 is computed, K while stage s - 2 is, whose last step forms the first scores of stage s - 1; both are asked
+    // for a stage before that.
+    constexpr bool kPipe = TPW <= 2;                 // (three tiles leave no registers for two generations of scores)
+    Held k_held = load(p.k, p.k_scale, 0), v_held = load(p.v, p.v_scale, 0), k_next{};
+    if constexpr (kPipe) k_next = load(p.k, p.k_scale, 1);
 
     // ---- query rows: tiles wr, wr + WR, ... of the row group ----
     const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
@@ -317,99 +333,211 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * GEO::KROW + GEO::k_piece(j, D == 128 ? qd : qd & 1) * 16;
     const uint32_t ks_take = GEO::K + GEO::K_BYTES + (j * NG + (qd & (NG - 1))) * 8;
     const uint32_t v_take = (wk * STEPS * 32 + 4 * qd + (j >> 2)) * kVRow<D> + (j & 3) * 8;
-    auto step = [&](auto i_tag, auto na_tag, const unsigned char *k_rows, uint2 words, const unsigned char *v_rows, int step_pos) {
-        constexpr int i = decltype(i_tag)::value, NA = decltype(na_tag)::value;
-        // scale bytes 2 i + kt of this key group's: of the two words all (WK 1), one (2), or half of one (4)
-        int word = WK == 1 ? (i < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
+    auto load_codes = [&](const unsigned char *k_rows, uint4 (&codes)[2]) {
+        codes[0] = *reinterpret_cast<const uint4 *>(k_rows);
+        codes[1] = *reinterpret_cast<const uint4 *>(k_rows + kPage * GEO::KROW);
+    };
+    auto load_v_frag = [&](const unsigned char *v_rows, int u) -> uint4 {
+        const uint2 lo = lds_read_tr16(v_rows + u * 32), hi = lds_read_tr16(v_rows + u * 32 + kPage * kVRow<D>);
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    };
+    // the word that holds scale bytes 2 i and 2 i + 1 of this key group: of the two all (WK 1), one (2), or half of one (4)
+    auto scale_word = [&](auto i_tag, uint2 words) -> int {
+        int word = WK == 1 ? (decltype(i_tag)::value < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
         if (WK == 4) word = (int)((uint32_t)word >> (16 * (wk & 1)));
-        const uint4 codes0 = *reinterpret_cast<const uint4 *>(k_rows + i * 32 * GEO::KROW);
-        const uint4 codes1 = *reinterpret_cast<const uint4 *>(k_rows + (i * 32 + kPage) * GEO::KROW);
-        const bool masked = step_pos + 32 > L;       // reaches drafts or the ragged end (uniform)
-        f32x4 s0, s1, n0, n1;
-        n0 = score<T, D, (2 * i) & 3>(codes0, word, q[0]);
-        n1 = score<T, D, (2 * i + 1) & 3>(codes1, word, q[0]);
-        uint4 pf[TPW];
+        return word;
+    };
+    auto scores = [&](auto i_tag, int t, const uint4 (&codes)[2], uint2 words, f32x4 (&s)[2]) {
+        constexpr int i = decltype(i_tag)::value;
+        const int word = scale_word(i_tag, words);
+        s[0] = score<T, D, (2 * i) & 3>(codes[0], word, q[t]);
+        s[1] = score<T, D, (2 * i + 1) & 3>(codes[1], word, q[t]);
+    };
+    auto mask = [&](f32x4 (&s)[2], int t, int step_pos) {
+        const int node = max(irow[t], 0);
+        uint64_t seen = ((uint64_t)__shfl((uint32_t)(anc >> 32), node) << 32) | __shfl((uint32_t)anc, node);
+        if (irow[t] < 0) seen = pos1 > L ? ~(uint64_t)0 >> (64 - Nb) : 0;       // a row without a node sees all of them
+        const int ahead = L - step_pos;              // prefix keys in this step (< 32), or minus the drafts before it
+        const uint32_t bits = ahead >= 0 ? ((1u << ahead) - 1u) | (uint32_t)(seen << ahead)
+                                         : (-ahead < 64 ? (uint32_t)(seen >> -ahead) : 0u);
+        const uint32_t va = bits >> (4 * qd), vb = va >> 16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            s[0][r] = (va >> r) & 1u ? s[0][r] : -INFINITY;
+            s[1][r] = (vb >> r) & 1u ? s[1][r] : -INFINITY;
+        }
+    };
+    auto exponents = [&](const f32x4 (&s)[2], int t, float (&x)[8]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            x[r] = __builtin_fmaf(s[0][r], q[t].c_log2, -m[t]);
+            x[4 + r] = __builtin_fmaf(s[1][r], q[t].c_log2, -m[t]);
+        }
+    };
+    auto highest = [](const float (&x)[8]) -> float {
+        return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    };
+    // moves the references of the rows that have a score above their room
+    auto move_reference = [&](const f32x4 (&s)[2], int t) {
+        const float all[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+        const float sc = quad_column_max(highest(all)) * q[t].c_log2;
+        const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
+        const float alpha = fast_exp2(m[t] - mn);
+        m[t] = mn;
+#pragma unroll
+        for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
+    };
+    // (the matrix pipe takes 16-bit weights; the row sum adds the same rounded ones)
+    auto weights = [&](float (&x)[8]) -> uint4 {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) x[r] = fast_exp2(x[r]);
+        return make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
+    };
+    const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
+
+    // Up to two tiles a wavefront.  S, the step's scores, are there already; the products that form those of the next step stand between this one's
+    // exponentials, and V's fragments are asked for before them.  A score above its row's room shows when the weights are formed, which are then
+    // formed again.
+    auto piped_step = [&](auto na_tag, f32x4 (&S)[TPW][2], f32x4 (&next)[TPW][2], const unsigned char *next_codes, auto next_tag, uint2 next_words,
+                          const unsigned char *v_rows, int step_pos) {
+        constexpr int NA = decltype(na_tag)::value;
+        uint4 codes[2], vf[NT], pf[TPW];
+        load_codes(next_codes, codes);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) vf[u] = load_v_frag(v_rows, u);
+        asm volatile("" ::: "memory");               // (no load sinks below)
+        if (step_pos + 32 > L)                       // reaches drafts or the ragged end (uniform)
+#pragma unroll
+            for (int t = 0; t < NA; ++t) mask(S[t], t, step_pos);
+        float x[NA][8], top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < NA; ++t) {
+            exponents(S[t], t, x[t]);
+            top = fmaxf(top, highest(x[t]));
+        }
+#pragma unroll
+        for (int t = 0; t < NA; ++t) scores(next_tag, t, codes, next_words, next[t]);
+#pragma unroll
+        for (int t = 0; t < NA; ++t) pf[t] = weights(x[t]);
+        if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {             // any lane's own keys can raise the alarm (uniform, rarely taken after the first step)
+#pragma unroll
+            for (int t = 0; t < NA; ++t) {
+                move_reference(S[t], t);
+                exponents(S[t], t, x[t]);
+                pf[t] = weights(x[t]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf[u], pf[t], O[t][u]);
+#pragma unroll
+        for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
+    };
+    // Three tiles: registers for one generation of scores, a tile's ahead of its softmax, and for a few of V's fragments.
+    constexpr int kAhead = 3;
+    auto plain_step = [&](auto i_tag, auto na_tag, const unsigned char *k_rows, uint2 words, const unsigned char *v_rows, int step_pos) {
+        constexpr int NA = decltype(na_tag)::value;
+        uint4 codes[2], vf[NT], pf[TPW];
+        load_codes(k_rows, codes);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) vf[u] = load_v_frag(v_rows, u);
+        asm volatile("" ::: "memory");
+        f32x4 s[2], next[2];
+        scores(i_tag, 0, codes, words, next);
         static_for<0, NA>([&](auto t_tag) {
             constexpr int t = decltype(t_tag)::value;
-            s0 = n0;
-            s1 = n1;
-            if (masked) {
-                const int node = max(irow[t], 0);
-                uint64_t seen = ((uint64_t)__shfl((uint32_t)(anc >> 32), node) << 32) | __shfl((uint32_t)anc, node);
-                if (irow[t] < 0) seen = pos1 > L ? ~(uint64_t)0 >> (64 - Nb) : 0;       // a row without a node sees all of them
-                const int ahead = L - step_pos;      // prefix keys in this step (< 32), or minus the drafts before it
-                const uint32_t bits = ahead >= 0 ? ((1u << ahead) - 1u) | (uint32_t)(seen << ahead)
-                                                 : (-ahead < 64 ? (uint32_t)(seen >> -ahead) : 0u);
-                const uint32_t va = bits >> (4 * qd), vb = va >> 16;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s0[r] = (va >> r) & 1u ? s0[r] : -INFINITY;
-                    s1[r] = (vb >> r) & 1u ? s1[r] : -INFINITY;
-                }
-            }
+            s[0] = next[0];
+            s[1] = next[1];
+            if (step_pos + 32 > L) mask(s, t, step_pos);
             float x[8];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -m[t]);
-                x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -m[t]);
+            exponents(s, t, x);
+            if (__builtin_amdgcn_ballot_w64(highest(x) > kGroupRoom<T>) != 0) {
+                move_reference(s, t);
+                exponents(s, t, x);
             }
-            // any lane's own keys can raise the alarm (uniform branch, rarely taken after the first step)
-            const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {
-                const float tm = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-                const float sc = quad_column_max(tm) * q[t].c_log2;
-                const float mn = sc > m[t] + kGroupRoom<T> ? sc : m[t];
-                const float alpha = fast_exp2(m[t] - mn);
-                m[t] = mn;
-#pragma unroll
-                for (int u = 0; u <= NT; ++u) O[t][u] *= alpha;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] = __builtin_fmaf(s0[r], q[t].c_log2, -mn);
-                    x[4 + r] = __builtin_fmaf(s1[r], q[t].c_log2, -mn);
-                }
-            }
-            if constexpr (t + 1 < NA) {              // the next tile's products beside this one's exponentials
-                n0 = score<T, D, (2 * i) & 3>(codes0, word, q[t + 1]);
-                n1 = score<T, D, (2 * i + 1) & 3>(codes1, word, q[t + 1]);
-            }
-#pragma unroll
-            for (int r = 0; r < 8; ++r) x[r] = fast_exp2(x[r]);
-            // (the matrix pipe takes 16-bit weights; the row sum adds the same rounded ones)
-            pf[t] = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
+            if constexpr (t + 1 < NA) scores(i_tag, t + 1, codes, words, next);
+            pf[t] = weights(x);
         });
-        const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const unsigned char *a = v_rows + i * 32 * kVRow<D> + u * 32;
-            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * kVRow<D>);
-            const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            if (u + kAhead < NT) vf[u + kAhead < NT ? u + kAhead : 0] = load_v_frag(v_rows, u + kAhead);
 #pragma unroll
-            for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
+            for (int t = 0; t < NA; ++t) O[t][u] = mfma16<T>(vf[u], pf[t], O[t][u]);
+            asm volatile("" ::: "memory");
         }
 #pragma unroll
         for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
     };
 
-    // ---- the loop: put stage s + 1, ask for stage s + 2, compute stage s ----
-    put(held, 0);
-    held = load(1);
+    // ---- the loop ----
+    put_k(k_held, 0);
+    put_v(v_held, 0);
+    v_held = load(p.v, p.v_scale, 1);
+    k_held = load(p.k, p.k_scale, kPipe ? 2 : 1);
+    if constexpr (kPipe) put_k(k_next, GEO::K_STAGE);
     __syncthreads();
     auto run = [&](auto na_tag) {
+        constexpr int NA = decltype(na_tag)::value;
+        using First = std::integral_constant<int, 0>;
+        f32x4 Sa[TPW][2], Sb[TPW][2];
+        uint2 words{};
+        if constexpr (kPipe && NA > 0) {
+            uint4 codes[2];
+            load_codes(smem + k_take, codes);
+            words = *reinterpret_cast<const uint2 *>(smem + ks_take);
+#pragma unroll
+            for (int t = 0; t < NA; ++t) scores(First{}, t, codes, words, Sa[t]);
+        }
+        uint32_t ring = 0;                           // of K
         for (int s = 0; s < stages; ++s) {
             const int buf = s & 1;
-            put(held, buf ^ 1);
-            if (((s + 2) & 63) == 0 && s + 2 < stages) pages = stage_pages(s + 2);
-            held = load(s + 2);
-            if constexpr (decltype(na_tag)::value > 0) {
-                const unsigned char *k_rows = smem + (k_take + buf * GEO::K_STAGE), *v_rows = smem + (v_take + buf * GEO::V_BYTES);
-                const uint2 words = *reinterpret_cast<const uint2 *>(smem + (ks_take + buf * GEO::K_STAGE));
-                const int pos = pos0 + s * kStage + wk * STEPS * 32;
-                static_for<0, STEPS>([&](auto i_tag) {
-                    constexpr int i = decltype(i_tag)::value;
-                    if (pos + i * 32 < pos1) step(i_tag, na_tag, k_rows, words, v_rows, pos + i * 32);       // uniform
-                });
+            const uint32_t ring1 = ring == 2 * GEO::K_STAGE ? 0 : ring + GEO::K_STAGE, ring2 = ring1 == 2 * GEO::K_STAGE ? 0 : ring1 + GEO::K_STAGE;
+            put_v(v_held, buf ^ 1);
+            if constexpr (kPipe) {
+                v_held = load(p.v, p.v_scale, s + 2);
+                put_k(k_held, ring2);
+                if (((s + 3) & 63) == 0 && s + 3 < stages) pages = stage_pages(s + 3);
+                k_held = load(p.k, p.k_scale, s + 3);
+            } else {
+                put_k(k_held, ring1);
+                if (((s + 2) & 63) == 0 && s + 2 < stages) pages = stage_pages(s + 2);
+                v_held = load(p.v, p.v_scale, s + 2);
+                k_held = load(p.k, p.k_scale, s + 2);
             }
+            if constexpr (NA > 0) {
+                const unsigned char *k_rows = smem + (k_take + ring), *k_rows1 = smem + (k_take + ring1), *v_rows = smem + (v_take + buf * GEO::V_BYTES);
+                const int pos = pos0 + s * kStage + wk * STEPS * 32;
+                if constexpr (kPipe) {
+                    const uint2 words1 = *reinterpret_cast<const uint2 *>(smem + (ks_take + ring1));
+                    static_for<0, STEPS>([&](auto i_tag) {
+                        constexpr int i = decltype(i_tag)::value;
+                        if (pos + i * 32 >= pos1) return;                        // uniform
+                        f32x4 (&now)[TPW][2] = i % 2 ? Sb : Sa, (&then)[TPW][2] = i % 2 ? Sa : Sb;
+                        // (the last step forms scores of what lies behind the end, for nobody)
+                        if constexpr (i + 1 < STEPS)
+                            piped_step(na_tag, now, then, k_rows + (i + 1) * 32 * GEO::KROW, std::integral_constant<int, i + 1>{}, words,
+                                       v_rows + i * 32 * kVRow<D>, pos + i * 32);
+                        else
+                            piped_step(na_tag, now, then, k_rows1, First{}, words1, v_rows + i * 32 * kVRow<D>, pos + i * 32);
+                    });
+                    words = words1;
+                    if constexpr (STEPS % 2 == 1)
+#pragma unroll
+                        for (int t = 0; t < NA; ++t) {
+                            Sa[t][0] = Sb[t][0];
+                            Sa[t][1] = Sb[t][1];
+                        }
+                } else {
+                    words = *reinterpret_cast<const uint2 *>(smem + (ks_take + ring));
+                    static_for<0, STEPS>([&](auto i_tag) {
+                        constexpr int i = decltype(i_tag)::value;
+                        if (pos + i * 32 < pos1)
+                            plain_step(i_tag, na_tag, k_rows + i * 32 * GEO::KROW, words, v_rows + i * 32 * kVRow<D>, pos + i * 32);     // uniform
+                    });
+                }
+            }
+            ring = ring1;
             __syncthreads();
         }
     };
@@ -797,8 +925,8 @@ static void launch_few_variant(const KParams &args, dim3 grid, hipStream_t s, hi
     OWL_GROUP_VARIANT(DT, T, D, 1, 2), OWL_GROUP_VARIANT(DT, T, D, 2, 2), OWL_GROUP_VARIANT(DT, T, D, 2, 4), OWL_GROUP_VARIANT(DT, T, D, 2, 8)
 
 static const Variant kGroupVariants[] = {
-    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 128), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 8),
-    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 64), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 4), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 8),
+    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 128), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 128, 3, 8),
+    OWL_GROUP_VARIANTS(OWL_BF16, __bf16, 64), OWL_GROUP_VARIANT(OWL_BF16, __bf16, 64, 3, 8),
     OWL_GROUP_VARIANTS(OWL_F16, _Float16, 128), OWL_GROUP_VARIANTS(OWL_F16, _Float16, 64),
     OWL_GROUP_FEWS(OWL_BF16, __bf16, 128), OWL_GROUP_FEWS(OWL_BF16, __bf16, 64), OWL_GROUP_FEWS(OWL_F16, _Float16, 128), OWL_GROUP_FEWS(OWL_F16, _Float16, 64),
 };
