@@ -84,20 +84,29 @@ owl_status check_quant_desc(const owl_verify_desc *d, Cached cached = Cached::kB
     return OWL_OK;
 }
 
-// The row tiles of a workgroup over 4-bit groups (owl_splitkv_groups.hip): as many as its wavefronts' registers hold, and fewer, in more row
-// groups, until the groups times the splits of cmin tokens fill three quarters of the compute units.
+// The row tiles of a workgroup over 4-bit groups, and how its wavefronts share the work (owl_splitkv_groups.hip).
 void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int *tpw, int *wr, int *wk, int *rgs, int *group_tiles)
 {
-    if (RT <= 4) {                                   // keys of a wavefront's own
-        // us, own keys / shared stages, 8 KV heads, 64K: 1 tile 21.0 / 28.6, 3 tiles 34.2 / 36.0, 4 tiles 34.7 / 36.9 (fp16 39.9 / 40.2), 7 and 8
-        // tiles 53.4 / 48.6 and 53.8 / 49.3; 16 sequences of 8K-64K, 1 tile 125 / 192, 2 tiles 146 / 198.
-        *rgs = (RT + 1) / 2;
-        *group_tiles = *tpw = (RT + *rgs - 1) / *rgs;
-        *wr = *rgs > 1 ? 2 : 1;
+    // Three ways.  us of a lone sequence of 8 KV heads, 4 query heads each, with 2-tile groups over shared stages / keys of a wavefront's own / groups
+    // of many tiles over shared stages:
+    //    2 tiles   1K 10.0 / 11.5     5K 11.4 / 12.5    16K 14.8 / 14.7    32K 19.4 / 17.9   128K 43.0 / 33.9
+    //    4 tiles   1K 10.6 / 11.7 / 13.9    5K 12.7 / 13.6 / 15.6    10K - / 15.9 / 17.6    64K - / 32.5 / 33.4   128K - / 52.5 / 51.5
+    //    8 tiles   1K 11.0 / 12.3 / 15.1    10K - / 18.5 / 20.1    16K - / 21.9 / 21.1     32K - / 32.4 / 29.3
+    //   15 tiles   1K 12.5 / 13.5 / 16.6    2K 14.4 / 15.0 / 16.9    10K - / 24.8 / 27.1   16K - / 32.0 / 28.2
+    // The first has little to set up, the second streams the cache, the third reads it least often.  Batches: 2 tiles, 16 of 5K 35.8 / 32.1, 16 of 8K-64K 180 / 136; 4 tiles, 16 of 5K - / 46.5 / 39.6, 16 of 8K-64K - / 242 / 226.
+    const int pairs = (RT + 1) / 2;
+    const int64_t tokens = d->batch * T * d->n_kv_heads / device_cus();          // of a compute unit, where every row is its own
+    const bool brief = RT > 1 && RT <= 16 && tokens * pairs <= 512, lone = d->batch == 1 && RT <= 16 && tokens <= (RT <= 4 ? 2560 : 384);
+    if (!brief && (pairs == 1 || lone)) {            // keys of a wavefront's own
+        *rgs = pairs;
+        *group_tiles = *tpw = (RT + pairs - 1) / pairs;
+        *wr = pairs > 1 ? 2 : 1;
         *wk = kWavesPerGroup;
         return;
     }
-    const int most = d->qkv_dtype == OWL_F16 ? 16 : 24;
+    // As many tiles as the wavefronts' registers hold (three parts of an fp16 query take more), and fewer until the groups times the splits of cmin
+    // tokens fill three quarters of the compute units.
+    const int most = brief ? 2 : d->qkv_dtype == OWL_F16 ? 16 : 24;
     int n = (RT + most - 1) / most;
     const int64_t least = d->split_tokens > 0 ? (int64_t)align_up((size_t)d->split_tokens, kSplitQuantum) : cmin;
     const int64_t splits = T <= least ? 1 : (T + least - 1) / least;

@@ -85,8 +85,21 @@ struct Query {
     float c_log2;
 };
 
+// The 16-byte pieces of a row that a lane takes
+template <int D> struct QueryRow { uint4 piece[D / 64][2]; };
+template <int D>
+__device__ __forceinline__ QueryRow<D> load_query(const unsigned char *row, int quad)
+{
+    QueryRow<D> r;
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) r.piece[h][c] = *reinterpret_cast<const uint4 *>(row + (64 * h + 16 * quad + 8 * c) * 2);
+    return r;
+}
+
 template <typename T, int D>
-__device__ __forceinline__ Query<T, D> take_query(const unsigned char *row, int quad, bool on, float c_log2)
+__device__ __forceinline__ Query<T, D> take_query(const QueryRow<D> &row, bool on, float c_log2)
 {
     using Q = Query<T, D>;
     constexpr int kHalves = D / 64;
@@ -96,7 +109,7 @@ __device__ __forceinline__ Query<T, D> take_query(const unsigned char *row, int 
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(row + (64 * h + 16 * quad + 8 * c) * 2);
+            const uint4 w = row.piece[h][c];
             const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -314,7 +327,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        q[t] = take_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd, irow[t] >= 0, p.c_log2);
+        q[t] = take_query<T, D>(load_query<D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd), irow[t] >= 0, p.c_log2);
     }
     const int my_tiles = max(0, (min(p.group_tiles, p.RT - rg * p.group_tiles) - wr + WR - 1) / WR);       // wave-uniform
     uint64_t anc = 0;                                // the drafts that node `lane` sees
@@ -691,6 +704,21 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     const int mine = max(0, (chunks - wave + kWaves - 1) / kWaves);
     unsigned char *ring = smem + wave * GEO::WAVE;
 
+    // ---- query rows: asked for before anything that waits for the pages ----
+    const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
+    const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * 2;
+    QueryRow<D> rows[TPW];
+    int irow[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+        const int tg = rg * p.group_tiles + t;
+        const bool tile_ok = t < p.group_tiles && tg < p.RT;
+        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
+        irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
+        const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
+        rows[t] = load_query<D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
+    }
+
     // Bad pages are page 0; behind the piece's end it is the piece's last one.
     const int last_lp = (pos1 - 1) / kPage, last_slot = (pos1 - 1) % kPage, lp0 = pos0 / kPage + wave * 2;
     auto checked = [&](int pg, int first) -> int {
@@ -729,20 +757,9 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     for (int d = 0; d < kDepth; ++d)
         if (d < mine) load(held[d], d);
 
-    // ---- query rows ----
-    const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
-    const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * 2;
     Query<T, D> q[TPW];
-    int irow[TPW];
 #pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-        const int tg = rg * p.group_tiles + t;
-        const bool tile_ok = t < p.group_tiles && tg < p.RT;
-        const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
-        irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
-        const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        q[t] = take_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd, irow[t] >= 0, p.c_log2);
-    }
+    for (int t = 0; t < TPW; ++t) q[t] = take_query<T, D>(rows[t], irow[t] >= 0, p.c_log2);
     uint64_t anc = 0;                                // the drafts that node `lane` sees
     if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
 
@@ -818,8 +835,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
         }
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const unsigned char *a = take_at + u * 32;
-            const uint2 lo = lds_read_tr16(a), hi = lds_read_tr16(a + kPage * GEO::VROW);
+            const uint2 lo = lds_read_tr16(take_at + u * 32), hi = lds_read_tr16(take_at + u * 32 + kPage * GEO::VROW);
             const uint4 vf = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
             for (int t = 0; t < TPW; ++t) O[t][u] = mfma16<T>(vf, pf[t], O[t][u]);
