@@ -157,3 +157,18 @@ def test_every_plan_has_a_kernel_that_covers_its_rows(group, dtype, D):
             per_group = -(-p.row_tiles // p.row_groups)
             assert 1 <= p.tiles_per_wave <= 3 and per_group <= 8 * p.tiles_per_wave
             assert p.split_tokens % 64 == 0 and p.split_tokens * p.max_splits >= ctx + n
+
+
+def test_every_kernel_is_some_calls():
+    taken = set()
+    for dtype in (B.OWL_BF16, B.OWL_F16):
+        for D in (64, 128):
+            for ctx in (1000, 20000, 131072):
+                for batch in (1, 16):
+                    for n in (1, 5, 16, 28, 48, 64):
+                        for group in (4, 8):
+                            d = B.make_desc(batch=batch, n_draft=n, n_q_heads=8 * group, n_kv_heads=8, head_dim=D, max_pages_per_seq=(ctx + n + 15) // 16,
+                                            max_ctx_len=ctx, qkv_dtype=dtype, scale=0.1, kv_stride_page=64 * D, kv_stride_head=8 * D, kv_stride_token=D // 2,
+                                            n_pool_pages=1 << 20, out_dtype=dtype)
+                            taken.add(B.owl_verify_attn_groups_plan(d).kernel_variant)
+    assert taken == set(range(59, 89))

@@ -119,6 +119,20 @@ def test_sequences_announced_as_long_ones(n, group, D, dtype):
 
 
 @pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [9, 16, 20, 28, 41, 60])
+def test_row_groups_with_keys_of_their_own(n, D, dtype):
+    """A lone sequence of two KV heads that may be 40000 long: up to eight groups of two row tiles."""
+    r = rng(n + 3 * D)
+    for ctx in (4500, 700, 31, 0):
+        gc = group_case("groups-own", n, dtype=dtype, Hq=8, Hkv=2, D=D, ctx_lens=[ctx], trees=_trees("tree", n, 1, r))
+        step = _announced(gc, 40000)
+        plan, tiles = B.owl_verify_attn_groups_plan(step.desc), (4 * n + 15) // 16
+        assert (plan.tiles_per_wave, plan.row_groups) == (2, (tiles + 1) // 2)
+        _check(step, gc, str(ctx))
+
+
+@pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
 def test_more_row_groups_than_an_xcd_has_compute_units(dtype):
     r = rng(9)
     gc = group_case("groups-rows", 9, dtype=dtype, Hq=32, Hkv=1, D=128, ctx_lens=[500], trees=_trees("tree", 64, 1, r))
