@@ -11,11 +11,17 @@
 //   values    O^T += V^T . P^T stays in 16 bits: the groups' scales lie along the channels, not along the keys that are summed over.
 //             V is widened once for all rows (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact), on its
 //             way into LDS, and read from there by the transposing read, as in the 16-bit pass.
-//   softmax   Each wavefront has a reference of its own for each row, which stays until a score lies more than kRoom above it and then
+//   softmax   Each wavefront has a reference of its own for each row, which stays until a score lies more than kGroupRoom above it and then
 //             moves to the row's highest score.
-// A stage is 128 tokens: each of the eight wavefronts brings one page of K and one of V, 16 bytes (8 for head_dim 64) and a scale byte a lane
-// of each, through registers, a stage ahead, into one of two buffers in LDS.  One barrier a stage.  The wavefronts are WR row groups of
-// TPW tiles times WK key groups, which take the 32-token steps of a stage in turn and merge at the end of a piece.
+// Two kernels.  Shared stages: 128 tokens at a time, of which each of the eight wavefronts brings one page of K and one of V, 16 bytes (8 for
+// head_dim 64) and a scale byte a lane of each, through registers: V into one of two buffers of LDS, widened, a stage ahead; K as it lies into a
+// ring of three, two stages ahead.  One barrier a stage.  The wavefronts are WR row groups of TPW tiles times WK key groups, which take the
+// 32-token steps of a stage in turn and merge at the end of a piece.  Keys of a wavefront's own, for few rows: further below.
+//
+// What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 121 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes
+// and scales); the products where rows are many, 153 us for 320 rows over 128K in bf16 (1.13 PFLOP/s counted as 16-bit products; fp16, with a part more of
+// each query, 197).  Between the two, 104 rows at 64K 42 us, in 16 sequences 316 (fp16 352): the matrix pipe works half of the time, a wavefront
+// issues for 35 % of its cycles, is ready without issuing for 35 % (its SIMD's pipe or other wavefront) and waits for 30 % (barrier, LDS, memory).
 #include "owl_splitkv.h"
 
 namespace owl {
@@ -670,9 +676,11 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
 // ---------------------------------------------------------------------------
 // Few rows: a wavefront shares nothing until the end of a piece.  The 32-token chunks of a piece are dealt to the eight wavefronts in turn; a
 // wavefront takes all rows of its row group, TPW tiles, against its own chunks.  K's codes and scale bytes go from memory into the
-// registers of the scaled product as they are (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 8 KB of LDS of the
-// wavefront's own and read back transposed, in order, without a barrier.  kDepth chunks of each tensor are on their way while one is computed.
-// At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
+// registers of the scaled product as they are (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 9 KB of LDS of the
+// wavefront's own and read back transposed, in order, without a barrier.  kDepth chunks of each tensor are on their way while one is computed (two:
+// three and four are no faster).  At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
+// Six nodes at 32K: 14 us and 4 for the combine, of which the loop, at the rate of memory, is 6; the rest is the way to the first chunk (lengths and
+// pages, then codes: two round trips), the merge and the partials.  Where the plan takes which: plan_groups in owl_api.hip, with both sides measured.
 // ---------------------------------------------------------------------------
 template <int D>
 struct OGeo {
