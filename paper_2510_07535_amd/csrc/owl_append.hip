@@ -312,11 +312,16 @@ __device__ __forceinline__ void store_groups(const Piece<T> &a, const Piece<T> &
 // ---------------------------------------------------------------------------
 // Append to a cache in the rows' own type, or (kFour) of 4-bit groups, which ask nothing of other tokens either: one workgroup per
 // token, an item a thread.  kNorm: with the norms of the heads.
+// Many tokens are bound by memory: a prompt of 8K in fp16, 201 MB, 45 us with the norms and 40 without (4.4 and 5.0 TB/s); four chunks of 2501
+// into 4 bits, 380 MB, 74 us (5.1 TB/s).  Few are bound by a workgroup's chain, lengths -> page, angles and products in 64 bits, of which an
+// item with the norm has some 200: with 384 threads, which 48 heads of 128 channels are in one pass, a tree of 60 tokens takes 4.5 us
+// and 16 trees of up to 26 into 4 bits 6.4; with 256 5.3 and 6.9, but of 1024 tokens 8.7 and 9.1 us, of 2048 14.8 and 13.6, of 8192 53 and 45.  (With the rows asked for before
+// the lengths, 5.5 and 7.0: they wait for nothing that the angles do not take as long as.)
 // ---------------------------------------------------------------------------
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kNormThreads = 384, kNormTokens = 768;
 
-template <typename T, int D, bool kPairs, bool kNorm, bool kFour>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs p)
+template <typename T, int D, bool kPairs, bool kNorm, bool kFour, int kThreads>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs p)
 {
     constexpr int E = Piece<T>::E, kItems = D / (2 * E), ES = sizeof(T);
     __shared__ double2 s_cs[D / 2];                          // [e][item]
@@ -334,11 +339,11 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
         const int t = p.pos_ids ? p.pos_ids[token] : at;
         s_cs[tid % E * turned + tid / E] = cos_sin((double)t * (double)p.inv_freq[tid], (double)p.rot_scale);
     }
-    if constexpr (kNorm) take_gains<D, kAppendThreads>(p, s_gain);
+    if constexpr (kNorm) take_gains<D, kThreads>(p, s_gain);
     __syncthreads();
     const int q_heads = p.q ? p.Hq : 0, heads = q_heads + 2 * p.Hkv;
     const int64_t row = (int64_t)page * p.stride_page + at % kPage * p.stride_token;
-    for (int id = tid; id < heads * kItems; id += kAppendThreads) {
+    for (int id = tid; id < heads * kItems; id += kThreads) {
         const int item = id % kItems, head = id / kItems;
         const int2 c = item_at<E, kPairs>(item, p.rot_dim);
         const unsigned char *from;
@@ -585,6 +590,17 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
     }
 }
 
+template <typename T, int D, bool kPairs, bool kNorm, bool kFour>
+static void launch_append_tokens(const AppendArgs &p, int B, hipStream_t s)
+{
+    if constexpr (kNorm)
+        if ((int64_t)p.n * B <= kNormTokens) {
+            hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, kFour, kNormThreads>), dim3(p.n, B), dim3(kNormThreads), 0, s, p);
+            return;
+        }
+    hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, kFour, kAppendThreads>), dim3(p.n, B), dim3(kAppendThreads), 0, s, p);
+}
+
 template <typename T, int D, bool kPairs, bool kNorm>
 static void launch_append_rows(const AppendArgs &p, int B, Cached cached, hipStream_t s)
 {
@@ -596,11 +612,11 @@ static void launch_append_rows(const AppendArgs &p, int B, Cached cached, hipStr
             return;
         }
         if (cached == Cached::kGroups4) {
-            hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, true>), dim3(p.n, B), dim3(kAppendThreads), 0, s, p);
+            launch_append_tokens<T, D, kPairs, kNorm, true>(p, B, s);
             return;
         }
     }
-    hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, false>), dim3(p.n, B), dim3(kAppendThreads), 0, s, p);
+    launch_append_tokens<T, D, kPairs, kNorm, false>(p, B, s);
 }
 
 template <typename T, int D>

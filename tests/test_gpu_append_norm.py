@@ -129,6 +129,16 @@ def test_rows_match_the_oracle(dtype, cache, norm, Hq, Hkv, D, ctx, n, rot_dim, 
 
 
 @pytest.mark.parametrize("dtype,cache,norm", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,D,ctx,n,rot_dim,pairs", [(3, 1, 128, [5], 768, 128, False), (3, 1, 128, [5], 769, 64, False), (7, 1, 64, [9, 0, 40], 300, 64, True),
+                                                          (20, 2, 128, [33, 1], 500, 128, True)])
+def test_many_tokens(dtype, cache, norm, Hq, Hkv, D, ctx, n, rot_dim, pairs):
+    a = Rows(n + D, dtype=dtype, cache=cache, norm=norm, Hq=Hq, Hkv=Hkv, D=D, ctx=ctx, n=n, rot_dim=rot_dim, pairs=pairs)
+    a.run()
+    a.check()
+    assert int(a.status.item()) == 0
+
+
+@pytest.mark.parametrize("dtype,cache,norm", KINDS)
 def test_far_positions_a_scale_and_no_gains(dtype, cache, norm):
     pos = np.array([[0, 131071, 1 << 20, (1 << 31) - 1, -5, 99999, 7], [3, 3, 4, 4, 5, 1 << 30, 1000003]], np.int64)
     a = Rows(3, dtype=dtype, cache=cache, norm=norm, gains=False, Hq=4, Hkv=2, D=128, ctx=[40, 7], n=7, rot_dim=128, pos=pos, rot_scale=1.1386)
