@@ -66,6 +66,16 @@ def test_batches_with_drafts_of_different_sizes(dtype, D, n, group, hkv, ctx, sp
         _check(step, gc, str(counts), counts)
 
 
+@pytest.mark.parametrize("dtype,D,n,group,hkv,ctx,split", [
+    (W.DT_BF16, 128, 16, 4, 2, 5000, 128), (W.DT_F16, 64, 28, 4, 8, 9000, 256), (W.DT_BF16, 128, 5, 4, 2, 3001, 64), (W.DT_BF16, 128, 40, 8, 2, 6000, 512),
+    (W.DT_F16, 128, 1, 8, 1, 2500, 192), (W.DT_BF16, 64, 60, 4, 4, 2111, 320),
+])
+def test_lone_sequences_in_equal_splits(dtype, D, n, group, hkv, ctx, split):
+    r = rng(ctx + n)
+    gc = group_case("groups-splits", 41 + n, dtype=dtype, Hq=hkv * group, Hkv=hkv, D=D, ctx_lens=[ctx], trees=_trees("tree", n, 1, r))
+    _check(GroupStep(gc, split_tokens=split), gc)
+
+
 @pytest.mark.parametrize("n,group,hkv,ctx", [(26, 4, 2, 20000), (60, 4, 2, 9000), (40, 8, 1, 30000), (6, 4, 1, 40000), (1, 4, 1, 70001)])
 @pytest.mark.parametrize("dtype", [W.DT_BF16, W.DT_F16])
 def test_long_contexts(n, group, hkv, ctx, dtype):
