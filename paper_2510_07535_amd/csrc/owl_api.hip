@@ -93,7 +93,8 @@ void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int 
     //    4 tiles   1K 10.6 / 11.7 / 13.9    5K 12.7 / 13.6 / 15.6    10K - / 15.9 / 17.6    64K - / 32.5 / 33.4   128K - / 52.5 / 51.5
     //    8 tiles   1K 11.0 / 12.3 / 15.1    10K - / 18.5 / 20.1    16K - / 21.9 / 21.1     32K - / 32.4 / 29.3
     //   15 tiles   1K 12.5 / 13.5 / 16.6    2K 14.4 / 15.0 / 16.9    10K - / 24.8 / 27.1   16K - / 32.0 / 28.2
-    // The first has little to set up, the second streams the cache, the third reads it least often.  Batches: 2 tiles, 16 of 5K 35.8 / 32.1, 16 of 8K-64K 180 / 136; 4 tiles, 16 of 5K - / 46.5 / 39.6, 16 of 8K-64K - / 242 / 226.
+    // The first has little to set up, the second streams the cache, the third reads it least often.  Batches: 2 tiles, 16 of 5K 35.8 / 32.1, 16 of
+    // 8K-64K 180 / 136; 4 tiles, 16 of 5K - / 46.5 / 39.6, 16 of 8K-64K - / 242 / 226.
     const int pairs = (RT + 1) / 2;
     const int64_t tokens = d->batch * T * d->n_kv_heads / device_cus();          // of a compute unit, where every row is its own
     const bool brief = RT > 1 && RT <= 16 && tokens * pairs <= 512, lone = d->batch == 1 && RT <= 16 && tokens <= (RT <= 4 ? 2560 : 384);
@@ -848,7 +849,8 @@ owl_status owl_gather_kv_groups(const owl_verify_desc *desc, const void *cache, 
 
 // ---- new rows of the cache ----
 static owl_status append_impl(const owl_verify_desc *desc, const owl_append_desc *a, const owl_norm_desc *norm, Cached cached,
-                              const void *q, const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache,
+                              const void *q, const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                              const int32_t *pos_ids, void *q_out, void *k_cache,
                               void *v_cache, uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table,
                               const int32_t *ctx_lens, const int32_t *n_new_seq, uint32_t *dev_status, void *stream)
 {

@@ -633,7 +633,8 @@ int64_t append_threads(int64_t n_tokens, Cached cached)
 }
 
 hipError_t launch_append(const owl_verify_desc &d, const owl_append_desc &a, const owl_norm_desc *norm, Cached cached, const void *q,
-                         const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq, const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
+                         const void *k_new, const void *v_new, const float *q_gain, const float *k_gain, const float *inv_freq,
+                         const int32_t *pos_ids, void *q_out, void *k_cache, void *v_cache,
                          uint8_t *k_scale, uint8_t *v_scale, const int32_t *page_table, const int32_t *ctx_lens,
                          const int32_t *n_new_seq, uint32_t *status, hipStream_t s)
 {
