@@ -79,16 +79,20 @@ __device__ __forceinline__ uint32_t quad_column_max_bits(uint32_t x)
     return max((uint32_t)r2[0], (uint32_t)r2[1]);
 }
 
-// A query tile as B operands of the scaled product: kParts e4m3 parts of the row's numbers over a power of two, which goes into the factor that takes
-// the row's products to the exponents of two, so that no size of q makes them overflow.  Lane (j, quad) holds row j;
+// A query tile as B operands of the scaled product: kParts e4m3 parts of the row's numbers over a power of two, 2^-up, which goes into the factor that
+// takes the row's products to the exponents of two, so that no size of q makes them overflow.  bf16: 2^up may be 2^126 where keys are up to 2^127.6, so the
+// product's own scale for the row takes up to 2^16 of it back.  128 products of 256 by 6 * 2^125 are then 2^126.6 at most, and where up is below 16 the sums are
+// those of q . k itself: a sum overflows only where it would in a 16-bit cache.  Lane (j, quad) holds row j;
 // the first half of an operand's 32 bytes are k = 16 quad .., the second k = 64 + 16 quad ...  With 64 channels the keys' codes stand at
 // k < 64 and again at k >= 64, and an operand's halves are two parts of the same channels.
 template <typename T, int D>
 struct Query {
     static constexpr int kParts = std::is_same<T, __bf16>::value ? 2 : 3;
     static constexpr int kOperands = D == 128 ? kParts : (kParts + 1) / 2;
+    static constexpr int kBack = std::is_same<T, __bf16>::value ? 16 : 0;        // (fp16: keys end at 2^16)
     i32x8 part[kOperands];
     float c_log2;
+    int scale;                                       // byte of the operand's power of two, biased by 127
 };
 
 // The 16-byte pieces of a row that a lane takes
@@ -139,10 +143,13 @@ __device__ __forceinline__ Query<T, D> take_query(const QueryRow<D> &row, bool o
     big = quad_column_max_bits(big);
     // The greatest becomes 128 .. 255, within e4m3's 448 however it is rounded; less where the row's factor would not be a normal number, for
     // products of 0 or -infinity by 0 or infinity are no numbers.  A number that is infinite or none makes the row's factor none.
-    const int least = 1 - (((int)(__builtin_bit_cast(uint32_t, c_log2) >> 23) & 255) - 127);
-    const int s = max((int)min(big >> 23, 254u) - 7, max(least, 1)), up = 127 - s;
+    const int e = (int)(__builtin_bit_cast(uint32_t, c_log2) >> 23) - 127;       // (c_log2 > 0)
+    const int s = max((int)min(big >> 23, 254u) - 7, max(1 - e - Q::kBack, 1)), up = 127 - s;
+    // (bf16: below 0 where the row's factor would be infinite otherwise, and the sums are the scores themselves over 2^127)
+    const int back = Q::kBack > 0 ? min(min(max(up, 0), Q::kBack), up - e + 127) : 0;
     Q q;
-    q.c_log2 = big >= 0x7F800000u ? __builtin_nanf("") : fminf(__builtin_ldexpf(c_log2, -up), FLT_MAX);
+    q.c_log2 = big >= 0x7F800000u ? __builtin_nanf("") : fminf(__builtin_ldexpf(c_log2, back - up), FLT_MAX);
+    q.scale = 127 - back;
     int bytes[Q::kParts][kHalves][4];
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
@@ -178,16 +185,27 @@ __device__ __forceinline__ Query<T, D> take_query(const QueryRow<D> &row, bool o
     return q;
 }
 
-// S += 16 keys' codes . 16 rows: the keys' scale byte is byte kByte of `k_scale`.
-template <typename T, int D, int kByte>
-__device__ __forceinline__ f32x4 score(const uint4 &codes, int k_scale, const Query<T, D> &q)
+// S += 16 keys' codes . 16 rows: the keys' scale byte is byte kByte of `k_scale`, the rows' byte kTile of `q_scales`.
+template <typename T, int D, int kByte, int kTile>
+__device__ __forceinline__ f32x4 score(const uint4 &codes, int k_scale, const Query<T, D> &q, int q_scales)
 {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     const i32x8 k = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
 #pragma unroll
     for (int o = 0; o < Query<T, D>::kOperands; ++o)
-        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, 0, 127);
+        if constexpr (Query<T, D>::kBack > 0) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, kTile, q_scales);
+        else s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, 0, 127);
     return s;
+}
+
+// The tiles' scale bytes in one register.
+template <typename T, int D, int TPW>
+__device__ __forceinline__ int pack_scales(const Query<T, D> (&q)[TPW])
+{
+    int scales = 0;
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) scales |= q[t].scale << (8 * t);
+    return scales;
 }
 
 // 4 or 2 words at an offset from a wave-uniform address; kOnce: no other row group reads them, and they are not kept (non-temporal).
@@ -335,6 +353,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
         q[t] = take_query<T, D>(load_query<D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd), irow[t] >= 0, p.c_log2);
     }
+    const int q_scales = pack_scales(q);
     const int my_tiles = max(0, (min(p.group_tiles, p.RT - rg * p.group_tiles) - wr + WR - 1) / WR);       // wave-uniform
     uint64_t anc = 0;                                // the drafts that node `lane` sees
     if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
@@ -366,11 +385,11 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         if (WK == 4) word = (int)((uint32_t)word >> (16 * (wk & 1)));
         return word;
     };
-    auto scores = [&](auto i_tag, int t, const uint4 (&codes)[2], uint2 words, f32x4 (&s)[2]) {
-        constexpr int i = decltype(i_tag)::value;
+    auto scores = [&](auto i_tag, auto t_tag, const uint4 (&codes)[2], uint2 words, f32x4 (&s)[2]) {
+        constexpr int i = decltype(i_tag)::value, t = decltype(t_tag)::value;
         const int word = scale_word(i_tag, words);
-        s[0] = score<T, D, (2 * i) & 3>(codes[0], word, q[t]);
-        s[1] = score<T, D, (2 * i + 1) & 3>(codes[1], word, q[t]);
+        s[0] = score<T, D, (2 * i) & 3, t>(codes[0], word, q[t], q_scales);
+        s[1] = score<T, D, (2 * i + 1) & 3, t>(codes[1], word, q[t], q_scales);
     };
     auto mask = [&](f32x4 (&s)[2], int t, int step_pos) {
         const int node = max(irow[t], 0);
@@ -435,8 +454,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
             exponents(S[t], t, x[t]);
             top = fmaxf(top, highest(x[t]));
         }
-#pragma unroll
-        for (int t = 0; t < NA; ++t) scores(next_tag, t, codes, next_words, next[t]);
+        static_for<0, NA>([&](auto t) { scores(next_tag, t, codes, next_words, next[decltype(t)::value]); });
 #pragma unroll
         for (int t = 0; t < NA; ++t) pf[t] = weights(x[t]);
         if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {             // any lane's own keys can raise the alarm (uniform, rarely taken after the first step)
@@ -464,7 +482,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         for (int u = 0; u < kAhead; ++u) vf[u] = load_v_frag(v_rows, u);
         asm volatile("" ::: "memory");
         f32x4 s[2], next[2];
-        scores(i_tag, 0, codes, words, next);
+        scores(i_tag, std::integral_constant<int, 0>{}, codes, words, next);
         static_for<0, NA>([&](auto t_tag) {
             constexpr int t = decltype(t_tag)::value;
             s[0] = next[0];
@@ -476,7 +494,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
                 move_reference(s, t);
                 exponents(s, t, x);
             }
-            if constexpr (t + 1 < NA) scores(i_tag, t + 1, codes, words, next);
+            if constexpr (t + 1 < NA) scores(i_tag, std::integral_constant<int, t + 1>{}, codes, words, next);
             pf[t] = weights(x);
         });
 #pragma unroll
@@ -506,8 +524,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
             uint4 codes[2];
             load_codes(smem + k_take, codes);
             words = *reinterpret_cast<const uint2 *>(smem + ks_take);
-#pragma unroll
-            for (int t = 0; t < NA; ++t) scores(First{}, t, codes, words, Sa[t]);
+            static_for<0, NA>([&](auto t) { scores(First{}, t, codes, words, Sa[decltype(t)::value]); });
         }
         uint32_t ring = 0;                           // of K
         for (int s = 0; s < stages; ++s) {
@@ -769,6 +786,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     Query<T, D> q[TPW];
 #pragma unroll
     for (int t = 0; t < TPW; ++t) q[t] = take_query<T, D>(rows[t], irow[t] >= 0, p.c_log2);
+    const int q_scales = pack_scales(q);
     uint64_t anc = 0;                                // the drafts that node `lane` sees
     if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
 
@@ -787,9 +805,10 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
         f32x4 S[TPW][2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int t = 0; t < TPW; ++t)
-                S[t][kt] = score<T, D, 0>(make_uint4(h.k[kt][0], h.k[kt][1], h.k[kt][2], h.k[kt][3]), (int)h.ks[kt], q[t]);
+            static_for<0, TPW>([&](auto t_tag) {
+                constexpr int t = decltype(t_tag)::value;
+                S[t][kt] = score<T, D, 0, t>(make_uint4(h.k[kt][0], h.k[kt][1], h.k[kt][2], h.k[kt][3]), (int)h.ks[kt], q[t], q_scales);
+            });
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const float scale = __builtin_bit_cast(float, h.vs[kt] << 23);           // (255: the conversion gives no numbers)
