@@ -695,8 +695,8 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
 // Few rows: a wavefront shares nothing until the end of a piece.  The 32-token chunks of a piece are dealt to the eight wavefronts in turn; a
 // wavefront takes all rows of its row group, TPW tiles, against its own chunks.  K's codes and scale bytes go from memory into the
 // registers of the scaled product as they are (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 9 KB of LDS of the
-// wavefront's own and read back transposed, in order, without a barrier.  kDepth chunks of each tensor are on their way while one is computed (two:
-// three and four are no faster).  At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
+// wavefront's own and read back transposed, in order, without a barrier.  Two chunks of each tensor are on their way while one is computed (three
+// and four are no faster).  At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
 // Six nodes at 32K: 14 us and 4 for the combine, of which the loop, at the rate of memory, is 6; the rest is the way to the first chunk (lengths and
 // pages, then codes: two round trips), the merge and the partials.  Where the plan takes which: plan_groups in owl_api.hip, with both sides measured.
 // ---------------------------------------------------------------------------
@@ -704,6 +704,7 @@ template <int D>
 struct OGeo {
     static constexpr int NT = D / 16, NG = D / 32, VROW = kVRow<D>, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
     static constexpr int CHUNK = 2 * kPage, WAVE = CHUNK * VROW;
+    static constexpr int DEPTH = 2;                              // chunks under way
     static constexpr int TILE = NT * 1024 + 512;
     static constexpr size_t LDS = (size_t)kWaves * (WAVE > TILE ? WAVE : TILE);
 };
@@ -718,12 +719,12 @@ __device__ __forceinline__ int own_chunk_pages(const KParams &p, int b, int pos0
     return p.page_table ? p.page_table[(int64_t)b * p.max_pages + min(lp, p.max_pages - 1)] : lp;
 }
 
-template <typename T, int D, int TPW, bool kOnce, int kDepth>
+template <typename T, int D, int TPW, bool kOnce>
 __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned char *smem, int wave, int lane, int g, int rg, const GPiece &pc,
                                               OwnPages ahead)
 {
     using GEO = OGeo<D>;
-    constexpr int NT = GEO::NT, NG = GEO::NG, LW = GEO::LW, CHUNK = GEO::CHUNK;
+    constexpr int NT = GEO::NT, NG = GEO::NG, LW = GEO::LW, CHUNK = GEO::CHUNK, kDepth = GEO::DEPTH;
     const int j = lane & 15, qd = lane >> 4, slot = lane >> 2, quarter = lane & 3;
     const int b = pc.b, L = pc.L, Nb = pc.Nb, pos0 = pc.pos0, pos1 = pc.pos1;
     const int chunks = (pos1 - pos0 + CHUNK - 1) / CHUNK;
@@ -932,29 +933,22 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_few_kernel(const Quan
     for_each_piece(
         p, [&](int, int, int b, int pos0) { ahead = OwnPages{own_chunk_pages(p, b, pos0, wave, lane, 0), pos0}; },
         [&](int g, int rg, const GPiece &pc) {
-            run_own_piece<T, D, TPW, kOnce, 2>(p, smem, wave, lane, g, rg, pc, ahead);
+            run_own_piece<T, D, TPW, kOnce>(p, smem, wave, lane, g, rg, pc, ahead);
             ahead.pos0 = -1;
         });
 }
 
+// (no entry point has events for these kernels)
 template <typename T, int D, int TPW, int WR>
-static void launch_groups_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t start, hipEvent_t stop)
+static void launch_groups_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t, hipEvent_t)
 {
-    const QuantParams &p = static_cast<const QuantParams &>(args);
-    if (start || stop)
-        hipExtLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, start, stop, 0, p);
-    else
-        hipLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, p);
+    hipLaunchKernelGGL((splitkv_groups_kernel<T, D, TPW, WR>), grid, dim3(kThreads), (GGeo<D, TPW, WR>::LDS), s, static_cast<const QuantParams &>(args));
 }
 
 template <typename T, int D, int TPW, bool kOnce>
-static void launch_few_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t start, hipEvent_t stop)
+static void launch_few_variant(const KParams &args, dim3 grid, hipStream_t s, hipEvent_t, hipEvent_t)
 {
-    const QuantParams &p = static_cast<const QuantParams &>(args);
-    if (start || stop)
-        hipExtLaunchKernelGGL((splitkv_groups_few_kernel<T, D, TPW, kOnce>), grid, dim3(kThreads), OGeo<D>::LDS, s, start, stop, 0, p);
-    else
-        hipLaunchKernelGGL((splitkv_groups_few_kernel<T, D, TPW, kOnce>), grid, dim3(kThreads), OGeo<D>::LDS, s, p);
+    hipLaunchKernelGGL((splitkv_groups_few_kernel<T, D, TPW, kOnce>), grid, dim3(kThreads), OGeo<D>::LDS, s, static_cast<const QuantParams &>(args));
 }
 
 // (wk = 8: keys of a wavefront's own; wr: 1, the only row group, or 2, one of several)
