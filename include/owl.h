@@ -477,10 +477,8 @@ owl_status owl_append_kv_groups(const owl_verify_desc *desc, const owl_append_de
                                 void *stream);
 
 /*
- * owl_verify_attn over a cache of 4-bit groups; q in desc->qkv_dtype, which is OWL_BF16 or OWL_F16.  Sums are in 32 bits.  The products of
- * queries and keys take a query as a sum of e4m3 numbers at the scale of its row, two (OWL_BF16) or three (OWL_F16) of them: exact down to 2^-9
- * (2^-6) of the row's greatest number, and off by at most 2^-17 of that below; the keys are exact, of whatever size: a row is no numbers only where its products
- * q.k, or those times scale, do not fit into 32 bits.  Weights are rounded to qkv_dtype before they meet the values.
+ * owl_verify_attn over a cache of 4-bit groups; q in desc->qkv_dtype, which is OWL_BF16 or OWL_F16.  Queries and keys are multiplied as they are, and sums are in
+ * 32 bits: a row is no numbers only where its products q.k, or those times scale, do not fit into them.  Weights are rounded to qkv_dtype before they meet the values.
  * fp16 queries, and calls with few rows, leave fp32 partials whether or not OWL_FLAG_FP32_PARTIALS asks for them.  Values (V) up to 2^80 are summed without overflow.
  * A query with a number that is infinite or none makes its row's answer no numbers, a key that is none those of the rows that see it, a value that is
  * none those of all rows of its sequence and KV head.

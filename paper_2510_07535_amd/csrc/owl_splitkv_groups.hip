@@ -1,16 +1,12 @@
 // Split-KV pass of the verify-step attention over a cache of 4-bit groups, for gfx950 (MI355X).
 //
-// The share of a workgroup, its pieces and their partials are those of owl_splitkv.h; the loop is another one, because the matrix pipe takes
-// 4-bit numbers with a scale for 32 of them as they lie in the cache:
-//   scores    S^T[key][row] = K . Q^T by v_mfma_scale_f32_16x16x128_f8f6f4, A = 16 keys' codes with their scale bytes: a lane holds the 32 channels
-//             of one group, 16 bytes, and its scale.  K is never widened.  B = Q as e4m3: a query is the sum of e4m3 numbers at one
-//             power of two for its row, x = hi + lo (+ lowest for fp16), hi the number rounded to four bits, lo the rest, again
-//             rounded, ...: two take bf16's eight bits, three fp16's eleven, exactly down to 2^-9 (2^-6) of the row's greatest, and to 2^-17 of
-//             that below.  One such product of 128 channels takes the pipe as long as two of 32 in 16 bits, so two are as
-//             cheap as the four that 16-bit keys need (measured on random operands: 70 and 112 instructions a us and SIMD).
-//   values    O^T += V^T . P^T stays in 16 bits: the groups' scales lie along the channels, not along the keys that are summed over.
-//             V is widened once for all rows (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact), on its
-//             way into LDS, and read from there by the transposing read, as in the 16-bit pass.
+// The share of a workgroup, its pieces and their partials are those of owl_splitkv.h; the loop is another one:
+//   scores    S^T[key][row] = K . Q^T by v_mfma_f32_16x16x32: A = 16 keys, of which a lane holds D / 4 channels as codes, 16 bytes (8) and a scale byte, and
+//             widens them in registers on their way into the product (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact).
+//             The pipe also takes codes as they lie (v_mfma_scale_f32_16x16x128_f8f6f4, with q as a sum of two or three e4m3 numbers), but not with sums
+//             in 32 bits: of 16 neighbouring channels it drops what lies 2^13 below the greatest product, measured.  Where one channel makes a score of 64
+//             the weights were off by 0.7 %, at 512 by 7 %.  With those products 60 rows of 4 heads over 64K take 63 us instead of 76, six 17.8 instead of 17.2.
+//   values    O^T += V^T . P^T.  V is widened once for all rows, on its way into LDS, and read from there by the transposing read, as in the 16-bit pass.
 //   softmax   Each wavefront has a reference of its own for each row, which stays until a score lies more than kGroupRoom above it and then
 //             moves to the row's highest score.
 // Two kernels.  Shared stages: 128 tokens at a time, of which each of the eight wavefronts brings one page of K and one of V, 16 bytes (8 for
@@ -19,14 +15,11 @@
 // 32-token steps of a stage in turn and merge at the end of a piece.  Keys of a wavefront's own, for few rows: further below.
 //
 // What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 121 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes
-// and scales); the products where rows are many, 153 us for 320 rows over 128K in bf16 (1.13 PFLOP/s counted as 16-bit products; fp16, with a part more of
-// each query, 197).  Between the two, 104 rows at 64K 42 us, in 16 sequences 316 (fp16 352): the matrix pipe works half of the time, a wavefront
-// issues for 35 % of its cycles, is ready without issuing for 35 % (its SIMD's pipe or other wavefront) and waits for 30 % (barrier, LDS, memory).
+// and scales); products, widening and softmax beside each other where rows are many, 162 us for 320 rows over 128K in bf16 (1.06 PFLOP/s).  Between the two, 104 rows
+// at 64K 49 us, in 16 sequences 364 (fp16 368).
 #include "owl_splitkv.h"
 
 namespace owl {
-
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStage = 128;                          // tokens of a stage
 
@@ -53,7 +46,7 @@ struct GGeo {
     static_assert(WR * WK == kWaves && STEPS >= 1, "eight wavefronts share four steps");
     static_assert(kWaves * TILE <= MAIN, "the merge fits the buffers");
     // Where a 16-byte piece of a row of K is, so that the fragment reads meet no bank twice.
-    static constexpr __host__ __device__ int k_piece(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 3) : piece ^ ((key >> 2) & 1); }
+    static constexpr __host__ __device__ int k_piece(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 3) : piece ^ ((key >> 3) & 1); }
 };
 
 // Two e2m1 codes, of byte `kByte` of a word, times a power of two, as two numbers of type T.
@@ -79,133 +72,77 @@ __device__ __forceinline__ uint32_t quad_column_max_bits(uint32_t x)
     return max((uint32_t)r2[0], (uint32_t)r2[1]);
 }
 
-// A query tile as B operands of the scaled product: kParts e4m3 parts of the row's numbers over a power of two, 2^-up, which goes into the factor that
-// takes the row's products to the exponents of two, so that no size of q makes them overflow.  bf16: 2^up may be 2^126 where keys are up to 2^127.6, so the
-// product's own scale for the row takes up to 2^16 of it back.  128 products of 256 by 6 * 2^125 are then 2^126.6 at most, and where up is below 16 the sums are
-// those of q . k itself: a sum overflows only where it would in a 16-bit cache.  Lane (j, quad) holds row j;
-// the first half of an operand's 32 bytes are k = 16 quad .., the second k = 64 + 16 quad ...  With 64 channels the keys' codes stand at
-// k < 64 and again at k >= 64, and an operand's halves are two parts of the same channels.
+// A query tile as B operands, and what takes its products to the exponents of two.  Lane (j, quad) holds the numbers of row j in channels quad D / 4 .., which
+// are those that the lane of key j has codes of: the products' k are the channels in another order, the same for both.
 template <typename T, int D>
 struct Query {
-    static constexpr int kParts = std::is_same<T, __bf16>::value ? 2 : 3;
-    static constexpr int kOperands = D == 128 ? kParts : (kParts + 1) / 2;
-    static constexpr int kBack = std::is_same<T, __bf16>::value ? 16 : 0;        // (fp16: keys end at 2^16)
-    i32x8 part[kOperands];
+    uint4 part[D / 32];
     float c_log2;
-    int scale;                                       // byte of the operand's power of two, biased by 127
 };
 
-// The 16-byte pieces of a row that a lane takes
-template <int D> struct QueryRow { uint4 piece[D / 64][2]; };
-template <int D>
-__device__ __forceinline__ QueryRow<D> load_query(const unsigned char *row, int quad)
-{
-    QueryRow<D> r;
-#pragma unroll
-    for (int h = 0; h < D / 64; ++h)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) r.piece[h][c] = *reinterpret_cast<const uint4 *>(row + (64 * h + 16 * quad + 8 * c) * 2);
-    return r;
-}
-
 template <typename T, int D>
-__device__ __forceinline__ Query<T, D> take_query(const QueryRow<D> &row, bool on, float c_log2)
+__device__ __forceinline__ Query<T, D> load_query(const unsigned char *row, int quad)
 {
-    using Q = Query<T, D>;
-    constexpr int kHalves = D / 64;
-    float x[kHalves][16];
-    uint32_t big = 0;
+    Query<T, D> q;
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const uint4 w = row.piece[h][c];
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float lo, hi;
-                if constexpr (std::is_same<T, __bf16>::value) {
-                    lo = __builtin_bit_cast(float, words[k] << 16);
-                    hi = __builtin_bit_cast(float, words[k] & 0xFFFF0000u);
-                } else {
-                    const f16x2 v = __builtin_bit_cast(f16x2, words[k]);
-                    lo = (float)v[0];
-                    hi = (float)v[1];
-                }
-                x[h][8 * c + 2 * k] = on ? lo : 0.f;
-                x[h][8 * c + 2 * k + 1] = on ? hi : 0.f;
-            }
-        }
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) big = max(big, __builtin_bit_cast(uint32_t, x[h][e]) & 0x7FFFFFFFu);
-    big = quad_column_max_bits(big);
-    // The greatest becomes 128 .. 255, within e4m3's 448 however it is rounded; less where the row's factor would not be a normal number, for
-    // products of 0 or -infinity by 0 or infinity are no numbers.  A number that is infinite or none makes the row's factor none.
-    const int e = (int)(__builtin_bit_cast(uint32_t, c_log2) >> 23) - 127;       // (c_log2 > 0)
-    const int s = max((int)min(big >> 23, 254u) - 7, max(1 - e - Q::kBack, 1)), up = 127 - s;
-    // (bf16: below 0 where the row's factor would be infinite otherwise, and the sums are the scores themselves over 2^127)
-    const int back = Q::kBack > 0 ? min(min(max(up, 0), Q::kBack), up - e + 127) : 0;
-    Q q;
-    q.c_log2 = big >= 0x7F800000u ? __builtin_nanf("") : fminf(__builtin_ldexpf(c_log2, back - up), FLT_MAX);
-    q.scale = 127 - back;
-    int bytes[Q::kParts][kHalves][4];
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            float rest[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) rest[e] = __builtin_ldexpf(x[h][4 * w + e], up);
-#pragma unroll
-            for (int part = 0; part < Q::kParts; ++part) {
-                int b = __builtin_amdgcn_cvt_pk_fp8_f32(rest[0], rest[1], 0, false);
-                b = __builtin_amdgcn_cvt_pk_fp8_f32(rest[2], rest[3], b, true);
-                bytes[part][h][w] = b;
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(b, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b, true);
-                rest[0] -= lo[0];
-                rest[1] -= lo[1];
-                rest[2] -= hi[0];
-                rest[3] -= hi[1];
-            }
-        }
-#pragma unroll
-    for (int o = 0; o < Q::kOperands; ++o)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if constexpr (D == 128) {
-                q.part[o][w] = bytes[o][0][w];
-                q.part[o][4 + w] = bytes[o][kHalves - 1][w];
-            } else {
-                q.part[o][w] = bytes[2 * o][0][w];
-                q.part[o][4 + w] = 2 * o + 1 < Q::kParts ? bytes[2 * o + 1 < Q::kParts ? 2 * o + 1 : 0][0][w] : 0;
-            }
-        }
+    for (int w = 0; w < D / 32; ++w) q.part[w] = *reinterpret_cast<const uint4 *>(row + (quad * (D / 4) + 8 * w) * 2);
     return q;
 }
 
-// S += 16 keys' codes . 16 rows: the keys' scale byte is byte kByte of `k_scale`, the rows' byte kTile of `q_scales`.
-template <typename T, int D, int kByte, int kTile>
-__device__ __forceinline__ f32x4 score(const uint4 &codes, int k_scale, const Query<T, D> &q, int q_scales)
+// Rows that are not there become zeros.  A number that is infinite or none makes its row's factor none.  A bf16 row with numbers above 2^100 is taken to that, and
+// its factor up, so that no size of q makes its products overflow (less where the factor would); what is lost lies 2^199 below.
+template <typename T, int D>
+__device__ __forceinline__ void take_query(Query<T, D> &q, bool on, float c_log2)
 {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    const i32x8 k = {(int)codes.x, (int)codes.y, (int)codes.z, (int)codes.w, 0, 0, 0, 0};
+    constexpr uint32_t kNone = std::is_same<T, __bf16>::value ? 0x7F80u : 0x7C00u;
+    uint32_t big = 0;
 #pragma unroll
-    for (int o = 0; o < Query<T, D>::kOperands; ++o)
-        if constexpr (Query<T, D>::kBack > 0) s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, kTile, q_scales);
-        else s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.part[o], s, 4, 0, kByte, k_scale, 0, 127);
-    return s;
+    for (int w = 0; w < D / 32; ++w) {
+        uint32_t *words = reinterpret_cast<uint32_t *>(&q.part[w]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            words[k] = on ? words[k] : 0u;
+            big = max(big, max(words[k] & 0x7FFFu, words[k] >> 16 & 0x7FFFu));
+        }
+    }
+    big = quad_column_max_bits(big);
+    q.c_log2 = big >= kNone ? __builtin_nanf("") : c_log2;
+    if constexpr (std::is_same<T, __bf16>::value) {
+        const int e = (int)(__builtin_bit_cast(uint32_t, c_log2) >> 23) - 127;       // (c_log2 > 0)
+        const int up = big >= kNone ? 0 : max(min(100 - ((int)(big >> 7) - 127), 0), e - 127);
+        if (__builtin_amdgcn_ballot_w64(up < 0) != 0) {
+            q.c_log2 = __builtin_ldexpf(q.c_log2, -up);
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+                uint32_t *words = reinterpret_cast<uint32_t *>(&q.part[w]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    words[k] = pack2<T>(__builtin_ldexpf(__builtin_bit_cast(float, words[k] << 16), up),
+                                        __builtin_ldexpf(__builtin_bit_cast(float, words[k] & 0xFFFF0000u), up));
+            }
+        }
+    }
 }
 
-// The tiles' scale bytes in one register.
-template <typename T, int D, int TPW>
-__device__ __forceinline__ int pack_scales(const Query<T, D> (&q)[TPW])
+// The scale of byte kByte of a word; 255 becomes infinity, from which the conversions make no numbers.
+template <int kByte>
+__device__ __forceinline__ float scale_of(uint32_t word)
 {
-    int scales = 0;
+    return __builtin_bit_cast(float, (kByte < 3 ? word << (23 - 8 * kByte) : word >> 1) & 0x7F800000u);
+}
+
+// s[t][kt] = 16 keys' codes . 16 rows of tile t, for kt = 0 or 1: what is widened serves all tiles.
+template <typename T, int D, int NA, int TPW>
+__device__ __forceinline__ void score(const uint32_t (&codes)[D / 32], float scale, const Query<T, D> (&q)[TPW], int kt, f32x4 (&s)[TPW][2])
+{
 #pragma unroll
-    for (int t = 0; t < TPW; ++t) scales |= q[t].scale << (8 * t);
-    return scales;
+    for (int t = 0; t < NA; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) {
+        const uint4 keys = widen_word<T>(codes[w], scale);
+#pragma unroll
+        for (int t = 0; t < NA; ++t) s[t][kt] = mfma16<T>(keys, q[t].part[w], s[t][kt]);
+    }
 }
 
 // 4 or 2 words at an offset from a wave-uniform address; kOnce: no other row group reads them, and they are not kept (non-temporal).
@@ -351,9 +288,9 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        q[t] = take_query<T, D>(load_query<D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd), irow[t] >= 0, p.c_log2);
+        q[t] = load_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
+        take_query(q[t], irow[t] >= 0, p.c_log2);
     }
-    const int q_scales = pack_scales(q);
     const int my_tiles = max(0, (min(p.group_tiles, p.RT - rg * p.group_tiles) - wr + WR - 1) / WR);       // wave-uniform
     uint64_t anc = 0;                                // the drafts that node `lane` sees
     if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
@@ -368,28 +305,38 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     }
 
     // ---- one step of 32 tokens ----
-    const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * GEO::KROW + GEO::k_piece(j, D == 128 ? qd : qd & 1) * 16;
-    const uint32_t ks_take = GEO::K + GEO::K_BYTES + (j * NG + (qd & (NG - 1))) * 8;
+    const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * GEO::KROW + (D == 128 ? GEO::k_piece(j, qd) * 16 : GEO::k_piece(j, qd >> 1) * 16 + (qd & 1) * 8);
+    const uint32_t ks_take = GEO::K + GEO::K_BYTES + (j * NG + (D == 128 ? qd : qd >> 1)) * 8;
     const uint32_t v_take = (wk * STEPS * 32 + 4 * qd + (j >> 2)) * kVRow<D> + (j & 3) * 8;
-    auto load_codes = [&](const unsigned char *k_rows, uint4 (&codes)[2]) {
-        codes[0] = *reinterpret_cast<const uint4 *>(k_rows);
-        codes[1] = *reinterpret_cast<const uint4 *>(k_rows + kPage * GEO::KROW);
+    struct Codes {
+        uint32_t key[2][LW];                         // of 16 keys each
+    };
+    auto load_codes = [&](const unsigned char *k_rows) -> Codes {
+        typedef typename std::conditional<LW == 4, Words4, Words2>::type Words;
+        Codes c;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const Words x = *reinterpret_cast<const Words *>(k_rows + kt * kPage * GEO::KROW);
+#pragma unroll
+            for (int w = 0; w < LW; ++w) c.key[kt][w] = x[w];
+        }
+        return c;
     };
     auto load_v_frag = [&](const unsigned char *v_rows, int u) -> uint4 {
         const uint2 lo = lds_read_tr16(v_rows + u * 32), hi = lds_read_tr16(v_rows + u * 32 + kPage * kVRow<D>);
         return make_uint4(lo.x, lo.y, hi.x, hi.y);
     };
     // the word that holds scale bytes 2 i and 2 i + 1 of this key group: of the two all (WK 1), one (2), or half of one (4)
-    auto scale_word = [&](auto i_tag, uint2 words) -> int {
-        int word = WK == 1 ? (decltype(i_tag)::value < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
-        if (WK == 4) word = (int)((uint32_t)word >> (16 * (wk & 1)));
+    auto scale_word = [&](auto i_tag, uint2 words) -> uint32_t {
+        uint32_t word = WK == 1 ? (decltype(i_tag)::value < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
+        if (WK == 4) word >>= 16 * (wk & 1);
         return word;
     };
-    auto scores = [&](auto i_tag, auto t_tag, const uint4 (&codes)[2], uint2 words, f32x4 (&s)[2]) {
-        constexpr int i = decltype(i_tag)::value, t = decltype(t_tag)::value;
-        const int word = scale_word(i_tag, words);
-        s[0] = score<T, D, (2 * i) & 3, t>(codes[0], word, q[t], q_scales);
-        s[1] = score<T, D, (2 * i + 1) & 3, t>(codes[1], word, q[t], q_scales);
+    auto scores = [&](auto i_tag, auto na_tag, const Codes &codes, uint2 words, f32x4 (&s)[TPW][2]) {
+        constexpr int i = decltype(i_tag)::value, NA = decltype(na_tag)::value;
+        const uint32_t word = scale_word(i_tag, words);
+        score<T, D, NA>(codes.key[0], scale_of<(2 * i) & 3>(word), q, 0, s);
+        score<T, D, NA>(codes.key[1], scale_of<(2 * i + 1) & 3>(word), q, 1, s);
     };
     auto mask = [&](f32x4 (&s)[2], int t, int step_pos) {
         const int node = max(irow[t], 0);
@@ -434,14 +381,13 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 
     // Up to two tiles a wavefront.  S, the step's scores, are there already; V's fragments and the next step's codes are asked for before the softmax, and the products
-    // that form the next scores run in one burst with those of the values, 26 of them, while the SIMD's other wavefront has its softmax.  (Woven into the exponentials
-    // instead, by hand, they make 104 rows at 64K 45-47 us for 43, 60 nodes 70-72 for 66.)  A score above its row's room shows when the weights are formed, which are then
+    // that form the next scores run in one burst with those of the values, 34 of them, while the SIMD's other wavefront has its softmax.  A score above its row's room shows when the weights are formed, which are then
     // formed again.
     auto piped_step = [&](auto na_tag, f32x4 (&S)[TPW][2], f32x4 (&next)[TPW][2], const unsigned char *next_codes, auto next_tag, uint2 next_words,
                           const unsigned char *v_rows, int step_pos) {
         constexpr int NA = decltype(na_tag)::value;
-        uint4 codes[2], vf[NT], pf[TPW];
-        load_codes(next_codes, codes);
+        uint4 vf[NT], pf[TPW];
+        const Codes codes = load_codes(next_codes);
 #pragma unroll
         for (int u = 0; u < NT; ++u) vf[u] = load_v_frag(v_rows, u);
         asm volatile("" ::: "memory");               // (no load sinks below)
@@ -454,7 +400,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
             exponents(S[t], t, x[t]);
             top = fmaxf(top, highest(x[t]));
         }
-        static_for<0, NA>([&](auto t) { scores(next_tag, t, codes, next_words, next[decltype(t)::value]); });
+        scores(next_tag, na_tag, codes, next_words, next);
 #pragma unroll
         for (int t = 0; t < NA; ++t) pf[t] = weights(x[t]);
         if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {             // any lane's own keys can raise the alarm (uniform, rarely taken after the first step)
@@ -472,31 +418,28 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
 #pragma unroll
         for (int t = 0; t < NA; ++t) O[t][NT] = mfma16<T>(ones, pf[t], O[t][NT]);
     };
-    // Three tiles: registers for one generation of scores, a tile's ahead of its softmax, and for a few of V's fragments.
+    // Three tiles: registers for one generation of scores, all of a step's ahead of the softmax, and for a few of V's fragments.
     constexpr int kAhead = 3;
     auto plain_step = [&](auto i_tag, auto na_tag, const unsigned char *k_rows, uint2 words, const unsigned char *v_rows, int step_pos) {
         constexpr int NA = decltype(na_tag)::value;
-        uint4 codes[2], vf[NT], pf[TPW];
-        load_codes(k_rows, codes);
+        uint4 vf[NT], pf[TPW];
+        const Codes codes = load_codes(k_rows);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) vf[u] = load_v_frag(v_rows, u);
         asm volatile("" ::: "memory");
-        f32x4 s[2], next[2];
-        scores(i_tag, std::integral_constant<int, 0>{}, codes, words, next);
-        static_for<0, NA>([&](auto t_tag) {
-            constexpr int t = decltype(t_tag)::value;
-            s[0] = next[0];
-            s[1] = next[1];
-            if (step_pos + 32 > L) mask(s, t, step_pos);
+        f32x4 s[TPW][2];
+        scores(i_tag, na_tag, codes, words, s);
+#pragma unroll
+        for (int t = 0; t < NA; ++t) {
+            if (step_pos + 32 > L) mask(s[t], t, step_pos);
             float x[8];
-            exponents(s, t, x);
+            exponents(s[t], t, x);
             if (__builtin_amdgcn_ballot_w64(highest(x) > kGroupRoom<T>) != 0) {
-                move_reference(s, t);
-                exponents(s, t, x);
+                move_reference(s[t], t);
+                exponents(s[t], t, x);
             }
-            if constexpr (t + 1 < NA) scores(i_tag, std::integral_constant<int, t + 1>{}, codes, words, next);
             pf[t] = weights(x);
-        });
+        }
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
             if (u + kAhead < NT) vf[u + kAhead < NT ? u + kAhead : 0] = load_v_frag(v_rows, u + kAhead);
@@ -521,10 +464,8 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         f32x4 Sa[TPW][2], Sb[TPW][2];
         uint2 words{};
         if constexpr (kPipe && NA > 0) {
-            uint4 codes[2];
-            load_codes(smem + k_take, codes);
             words = *reinterpret_cast<const uint2 *>(smem + ks_take);
-            static_for<0, NA>([&](auto t) { scores(First{}, t, codes, words, Sa[decltype(t)::value]); });
+            scores(First{}, na_tag, load_codes(smem + k_take), words, Sa);
         }
         uint32_t ring = 0;                           // of K
         for (int s = 0; s < stages; ++s) {
@@ -694,7 +635,7 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
 // ---------------------------------------------------------------------------
 // Few rows: a wavefront shares nothing until the end of a piece.  The 32-token chunks of a piece are dealt to the eight wavefronts in turn; a
 // wavefront takes all rows of its row group, TPW tiles, against its own chunks.  K's codes and scale bytes go from memory into the
-// registers of the scaled product as they are (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 9 KB of LDS of the
+// registers of the lanes that widen them (16 keys of 64 bytes are 64 lanes' 16 bytes); V is widened into 9 KB of LDS of the
 // wavefront's own and read back transposed, in order, without a barrier.  Two chunks of each tensor are on their way while one is computed (three
 // and four are no faster).  At the end the wavefronts' sums meet in LDS, a channel tile a wavefront, and leave one partial in fp32.
 // Six nodes at 32K: 14 us and 4 for the combine, of which the loop, at the rate of memory, is 6; the rest is the way to the first chunk (lengths and
@@ -734,7 +675,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     // ---- query rows: asked for before anything that waits for the pages ----
     const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
     const unsigned char *q_head = static_cast<const unsigned char *>(p.q) + ((int64_t)b * p.N * p.Hq + (int64_t)g * p.G) * D * 2;
-    QueryRow<D> rows[TPW];
+    Query<T, D> q[TPW];
     int irow[TPW];
 #pragma unroll
     for (int t = 0; t < TPW; ++t) {
@@ -743,7 +684,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
         const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        rows[t] = load_query<D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
+        q[t] = load_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
     }
 
     // Bad pages are page 0; behind the piece's end it is the piece's last one.
@@ -760,12 +701,12 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
 
     // ---- transfers ----
     struct Held {
-        uint32_t k[2][4], v[2][LW], ks[2], vs[2];
+        uint32_t k[2][LW], v[2][LW], ks[2], vs[2];
     };
     Held held[kDepth];
     const int64_t head_off = (int64_t)g * p.stride_head;
     const uint32_t tok = (uint32_t)p.stride_token;
-    const uint32_t k_piece = (uint32_t)((qd & (NG - 1)) * 16), v_piece = (uint32_t)(quarter * LW * 4), ks_piece = qd & (NG - 1), vs_piece = D == 128 ? quarter : quarter >> 1;
+    const uint32_t k_piece = (uint32_t)(qd * LW * 4), v_piece = (uint32_t)(quarter * LW * 4), ks_piece = D == 128 ? qd : qd >> 1, vs_piece = D == 128 ? quarter : quarter >> 1;
     const uint32_t k_slot = (uint32_t)j * tok, v_slot = (uint32_t)slot * tok, ks_slot = (uint32_t)(j * NG), vs_slot = (uint32_t)(slot * NG);
     auto load = [&](Held &h, int i) {
 #pragma unroll
@@ -774,7 +715,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
             const int most = lp0 + i * (2 * kWaves) + t < last_lp ? kPage - 1 : last_slot;      // rows past the end: the last one again, masked later
             const uint32_t bytes = (uint32_t)most * tok, scales = (uint32_t)(most * NG);
             const int64_t s_at = (page * p.Hkv + g) * (kPage * NG);
-            load_words<4, kOnce>(h.k[t], static_cast<const unsigned char *>(p.k) + at, min(k_slot, bytes) + k_piece);
+            load_words<LW, kOnce>(h.k[t], static_cast<const unsigned char *>(p.k) + at, min(k_slot, bytes) + k_piece);
             h.ks[t] = (p.k_scale + s_at)[min(ks_slot, scales) + ks_piece];
             load_words<LW, kOnce>(h.v[t], static_cast<const unsigned char *>(p.v) + at, min(v_slot, bytes) + v_piece);
             h.vs[t] = (p.v_scale + s_at)[min(vs_slot, scales) + vs_piece];
@@ -784,10 +725,8 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     for (int d = 0; d < kDepth; ++d)
         if (d < mine) load(held[d], d);
 
-    Query<T, D> q[TPW];
 #pragma unroll
-    for (int t = 0; t < TPW; ++t) q[t] = take_query<T, D>(rows[t], irow[t] >= 0, p.c_log2);
-    const int q_scales = pack_scales(q);
+    for (int t = 0; t < TPW; ++t) take_query(q[t], irow[t] >= 0, p.c_log2);
     uint64_t anc = 0;                                // the drafts that node `lane` sees
     if (pos1 > L) anc = ancestor_sets(p.parent[(int64_t)b * p.N + min(lane, p.N - 1)], lane, Nb, p.dev_status);
 
@@ -805,11 +744,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     auto step = [&](Held &h, int i, auto more_tag) {
         f32x4 S[TPW][2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-            static_for<0, TPW>([&](auto t_tag) {
-                constexpr int t = decltype(t_tag)::value;
-                S[t][kt] = score<T, D, 0, t>(make_uint4(h.k[kt][0], h.k[kt][1], h.k[kt][2], h.k[kt][3]), (int)h.ks[kt], q[t], q_scales);
-            });
+        for (int kt = 0; kt < 2; ++kt) score<T, D, TPW>(h.k[kt], __builtin_bit_cast(float, h.ks[kt] << 23), q, kt, S);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const float scale = __builtin_bit_cast(float, h.vs[kt] << 23);           // (255: the conversion gives no numbers)

@@ -67,8 +67,8 @@ def test_rows_of_different_sizes_against_great_keys(layout, q_exp, k_exp, scale_
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("layout", list(LAYOUTS))
 def test_a_great_channel_that_no_key_has(layout, D):
-    """Queries of 2^113 .. 2^114, exact in two parts beside one channel of 2^122, which is 0 in all keys; the keys' others are 0 or 2^-126; a scale of 2^15.
-    The scores are some dozens, and the scale times the row's power of two is beyond 2^128."""
+    """Queries of 2^113 .. 2^114 but for one channel of 2^122, which is 0 in all keys; the keys' others are 0 or 2^-126; a scale of 2^15.  The scores are
+    some dozens."""
     step, gc = _step(layout, D, 0, 0, 0)
     c, r = gc.case, rng(D)
     step.desc.scale = c.scale = 2.0 ** 15
@@ -82,5 +82,38 @@ def test_a_great_channel_that_no_key_has(layout, D):
     c.q[...] = W.store((r.choice([-1.0, 1.0], c.q.shape) * r.uniform(1.0, 1.99, c.q.shape) * 2.0 ** 113).astype(np.float32), W.DT_BF16)
     c.q[..., 0] = W.store(np.full(1, 2.0 ** 122, np.float32), W.DT_BF16)
     step.q.copy_(_to_dev(c.q, DEV))
+    assert_attention(step.result(), gc, oracle_out(gc), layout)
+    assert int(step.status.item()) == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,above", [(W.DT_BF16, 7), (W.DT_BF16, 9), (W.DT_BF16, 10), (W.DT_BF16, 12), (W.DT_F16, 4), (W.DT_F16, 6), (W.DT_F16, 9), (W.DT_F16, 12)])
+@pytest.mark.parametrize("layout", [k for k in LAYOUTS if k != "shared, 20 tiles"])
+def test_channels_far_below_their_rows_greatest(layout, dtype, above, D):
+    """One channel of q is 2^above greater than the others, with keys that are all 1 there, so that the others' products decide."""
+    n, group, announced, own, tiles, groups = LAYOUTS[layout]
+    r = rng(n + above + D)
+    gc = group_case("groups-channels", n, dtype=dtype, Hq=2 * group, Hkv=2, D=D, ctx_lens=[900], trees=[W.random_tree(n, 6, r)])
+    c, hot = gc.case, 37
+    byte, scale = gc.raw[0][..., hot // 2], gc.scale[0][..., hot // 32]
+    fine = scale != 255
+    code = np.zeros(scale.shape, np.uint8)
+    for e, k in ((-2, 6), (-1, 4), (0, 2)):                              # 1 as 4 / 4, 2 / 2, 1
+        code[scale == 127 + e] = k
+    assert (code[fine] > 0).all()
+    byte[fine] = (byte[fine] & 15) | code[fine] << 4                     # (an odd channel: the upper half)
+    c.k_pool[..., hot][fine] = W.store(np.ones(1, np.float32), dtype)
+    q = W.widen(c.q, dtype)
+    q[..., hot] = np.sign(q[..., hot]) * 2.0 ** above
+    c.q[...] = W.store(q.astype(np.float32), dtype)
+    step = GroupStep(gc, max_ctx_len=announced)
+    if announced is not None:
+        wide = (announced + n + 15) // 16
+        table = np.full((1, wide), -1, np.int32)
+        table[:, :c.page_table.shape[1]] = c.page_table
+        step.table, step.desc.max_pages_per_seq = i32(table), wide
+        step.ws = torch.full((B.owl_verify_attn_groups_workspace_size(step.desc),), 0xFF, dtype=torch.uint8, device=DEV)
+    plan = B.owl_verify_attn_groups_plan(step.desc)
+    assert (plan.kernel_variant >= FIRST_OWN, plan.tiles_per_wave, plan.row_groups) == (own, tiles, groups)
     assert_attention(step.result(), gc, oracle_out(gc), layout)
     assert int(step.status.item()) == 0
