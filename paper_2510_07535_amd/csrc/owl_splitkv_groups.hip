@@ -1,22 +1,24 @@
 // Split-KV pass of the verify-step attention over a cache of 4-bit groups, for gfx950 (MI355X).
 //
 // The share of a workgroup, its pieces and their partials are those of owl_splitkv.h; the loop is another one:
-//   scores    S^T[key][row] = K . Q^T by v_mfma_f32_16x16x32: A = 16 keys, of which a lane holds D / 4 channels as codes, 16 bytes (8) and a scale byte, and
-//             widens them in registers on their way into the product (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact).
+//   scores    S^T[key][row] = K . Q^T by v_mfma_f32_16x16x32 on widened keys (v_cvt_scalef32_pk_*_fp4: two numbers an instruction, scale applied, exact).
 //             The pipe also takes codes as they lie (v_mfma_scale_f32_16x16x128_f8f6f4, with q as a sum of two or three e4m3 numbers), but not with sums
-//             in 32 bits: of 16 neighbouring channels it drops what lies 2^13 below the greatest product, measured.  Where one channel makes a score of 64
-//             the weights were off by 0.7 %, at 512 by 7 %.  With those products 60 rows of 4 heads over 64K take 63 us instead of 76, six 17.8 instead of 17.2.
-//   values    O^T += V^T . P^T.  V is widened once for all rows, on its way into LDS, and read from there by the transposing read, as in the 16-bit pass.
+//             in 32 bits: of 16 neighbouring channels it drops what lies 2^13 below the greatest product (measured; the 16-bit product drops nothing there).
+//             Where one channel makes a score of 64 the weights were off by 0.7 %, at 512 by 7 %.  (With those products 240 rows over 64K take 65 us
+//             instead of 69, 320 over 128K 152 instead of 162, in fp16 77 instead of 71 and 197 instead of 195.)
+//   values    O^T += V^T . P^T, V read from LDS by the transposing read, as in the 16-bit pass.
 //   softmax   Each wavefront has a reference of its own for each row, which stays until a score lies more than kGroupRoom above it and then
 //             moves to the row's highest score.
 // Two kernels.  Shared stages: 128 tokens at a time, of which each of the eight wavefronts brings one page of K and one of V, 16 bytes (8 for
-// head_dim 64) and a scale byte a lane of each, through registers: V into one of two buffers of LDS, widened, a stage ahead; K as it lies into a
-// ring of three, two stages ahead.  One barrier a stage.  The wavefronts are WR row groups of TPW tiles times WK key groups, which take the
-// 32-token steps of a stage in turn and merge at the end of a piece.  Keys of a wavefront's own, for few rows: further below.
+// head_dim 64) and a scale byte a lane of each, through registers, and widens them into LDS a stage ahead: two buffers of each.  One barrier a stage.
+// (Each wavefront widening the codes of K that it multiplies, from a third of the bytes in LDS: 240 rows over 64K 77 instead of 69 us, 104 49 instead of 47.)
+// The wavefronts are WR row groups of TPW tiles times WK key groups, which take the 32-token steps of a stage in turn and merge at the end of a piece.
+// Keys of a wavefront's own, for few rows: further below.
 //
-// What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 121 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes
-// and scales); products, widening and softmax beside each other where rows are many, 162 us for 320 rows over 128K in bf16 (1.06 PFLOP/s).  Between the two, 104 rows
-// at 64K 49 us, in 16 sequences 364 (fp16 368).
+// What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 120 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes
+// and scales); products, fragments from LDS and softmax beside each other where rows are many, 162 us for 320 rows over 128K in bf16 (1.06 PFLOP/s; fp16, in
+// two row groups, 195).  Between the two, 104 rows at 64K 47 us, in 16 sequences 365 (fp16 370): 16 KB of fragments from LDS take as long as the 34 products
+// that two tiles make of them.
 #include "owl_splitkv.h"
 
 namespace owl {
@@ -27,26 +29,22 @@ constexpr int kStage = 128;                          // tokens of a stage
 template <typename T> constexpr float kGroupRoom = 11.0f;
 template <> constexpr float kGroupRoom<__bf16> = 24.0f;
 
-// A row of widened V in LDS, padded so that neither the transposing reads, 32 bytes of 8 rows at a time, nor the stores meet a bank twice, and so that all
-// fragments are at fixed distances from one address.
-template <int D> constexpr int kVRow = 2 * D + 32;
+// A row of widened K or V in LDS, padded so that neither the reads, of V transposing, 32 bytes of 8 rows at a time, of K 16 bytes, nor the stores meet a bank
+// twice, and so that all fragments are at fixed distances from one address.
+template <int D> constexpr int kRow = 2 * D + 32;
 
 template <int D, int TPW, int WR>
 struct GGeo {
     static constexpr int WK = kWaves / WR, STEPS = 4 / WK;       // key groups; 32-token steps of a stage that each takes
     static constexpr int NG = D / 32;                            // groups of a row
     static constexpr int LB = D / 8, LW = LB / 4;                // bytes (words) of a page of one tensor that a lane brings
-    static constexpr int KROW = D / 2;                           // bytes of a row of K's codes
-    static constexpr int K_BYTES = kStage * KROW, K_STAGE = K_BYTES + kPage * NG * 8;      // a stage of K: codes, then scales as [slot][group][page]
-    static constexpr int V_BYTES = kStage * kVRow<D>;
-    static constexpr int K = 2 * V_BYTES, MAIN = K + 3 * K_STAGE;        // two stages of V, then three of K
+    static constexpr int T_BYTES = kStage * kRow<D>;            // a stage of K or of V, widened
+    static constexpr int K = 2 * T_BYTES, MAIN = 4 * T_BYTES;    // two stages of V, then two of K
     static constexpr int NT = D / 16;                            // channel tiles of O^T
     static constexpr int TILE = NT * 1024 + 512;                 // a wavefront's part of a tile in the merge
     static constexpr size_t LDS = MAIN;
     static_assert(WR * WK == kWaves && STEPS >= 1, "eight wavefronts share four steps");
     static_assert(kWaves * TILE <= MAIN, "the merge fits the buffers");
-    // Where a 16-byte piece of a row of K is, so that the fragment reads meet no bank twice.
-    static constexpr __host__ __device__ int k_piece(int key, int piece) { return D == 128 ? piece ^ ((key >> 1) & 3) : piece ^ ((key >> 3) & 1); }
 };
 
 // Two e2m1 codes, of byte `kByte` of a word, times a power of two, as two numbers of type T.
@@ -72,20 +70,20 @@ __device__ __forceinline__ uint32_t quad_column_max_bits(uint32_t x)
     return max((uint32_t)r2[0], (uint32_t)r2[1]);
 }
 
-// A query tile as B operands, and what takes its products to the exponents of two.  Lane (j, quad) holds the numbers of row j in channels quad D / 4 .., which
-// are those that the lane of key j has codes of: the products' k are the channels in another order, the same for both.
+// A query tile as B operands, and what takes its products to the exponents of two.  Lane (j, quad) holds numbers of row j, eight for each product; kOwn: those of
+// channels quad D / 4 .., which are the ones that the lane of key j has codes of.  (The products' k are the channels in any order that is the same for both.)
 template <typename T, int D>
 struct Query {
     uint4 part[D / 32];
     float c_log2;
 };
 
-template <typename T, int D>
+template <typename T, int D, bool kOwn>
 __device__ __forceinline__ Query<T, D> load_query(const unsigned char *row, int quad)
 {
     Query<T, D> q;
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w) q.part[w] = *reinterpret_cast<const uint4 *>(row + (quad * (D / 4) + 8 * w) * 2);
+    for (int w = 0; w < D / 32; ++w) q.part[w] = *reinterpret_cast<const uint4 *>(row + (kOwn ? quad * (D / 4) + 8 * w : 32 * w + 8 * quad) * 2);
     return q;
 }
 
@@ -124,24 +122,17 @@ __device__ __forceinline__ void take_query(Query<T, D> &q, bool on, float c_log2
     }
 }
 
-// The scale of byte kByte of a word; 255 becomes infinity, from which the conversions make no numbers.
-template <int kByte>
-__device__ __forceinline__ float scale_of(uint32_t word)
-{
-    return __builtin_bit_cast(float, (kByte < 3 ? word << (23 - 8 * kByte) : word >> 1) & 0x7F800000u);
-}
-
-// s[t][kt] = 16 keys' codes . 16 rows of tile t, for kt = 0 or 1: what is widened serves all tiles.
-template <typename T, int D, int NA, int TPW>
+// s[t][kt] = 16 keys' codes . 16 rows of tile t, for kt = 0 or 1, widened in registers: what is widened serves all tiles.
+template <typename T, int D, int TPW>
 __device__ __forceinline__ void score(const uint32_t (&codes)[D / 32], float scale, const Query<T, D> (&q)[TPW], int kt, f32x4 (&s)[TPW][2])
 {
 #pragma unroll
-    for (int t = 0; t < NA; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < TPW; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {
         const uint4 keys = widen_word<T>(codes[w], scale);
 #pragma unroll
-        for (int t = 0; t < NA; ++t) s[t][kt] = mfma16<T>(keys, q[t].part[w], s[t][kt]);
+        for (int t = 0; t < TPW; ++t) s[t][kt] = mfma16<T>(keys, q[t].part[w], s[t][kt]);
     }
 }
 
@@ -249,19 +240,12 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         h.scale = (scales + lane_of(pages.scales, s & 63))[min(slot_scale, (uint32_t)(most * NG)) + group];
         return h;
     };
-    // ... and into LDS: codes of K, their scale bytes as [slot][group][page]; V in 16 bits, whose 16-byte pieces the lanes of the upper half
-    // of a row store in another order, so that eight lanes meet no bank twice
+    // ... and into LDS, in 16 bits: the lanes of the upper half of a row store its 16-byte pieces in another order, so that eight lanes meet no bank twice
     const int key = wave * kPage + slot, turn = D == 128 ? quarter >> 1 : 0;
-    const uint32_t k_put = GEO::K + key * GEO::KROW + (D == 128 ? GEO::k_piece(key, quarter) * 16 : GEO::k_piece(key, quarter >> 1) * 16 + (quarter & 1) * 8);
-    const uint32_t ks_put = GEO::K + GEO::K_BYTES + (slot * NG + group) * 8 + wave, v_put = key * kVRow<D> + quarter * LW * 16;
-    auto put_k = [&](const Held &h, uint32_t ring) {
-        if constexpr (LW == 4) *reinterpret_cast<uint4 *>(smem + (k_put + ring)) = make_uint4(h.words[0], h.words[1], h.words[2], h.words[3]);
-        else *reinterpret_cast<uint2 *>(smem + (k_put + ring)) = make_uint2(h.words[0], h.words[1]);
-        smem[ks_put + ring] = (uint8_t)h.scale;
-    };
-    auto put_v = [&](const Held &h, int buf) {
+    const uint32_t put_at = key * kRow<D> + quarter * LW * 16;
+    auto put = [&](const Held &h, uint32_t buffer) {
         const float scale = __builtin_bit_cast(float, h.scale << 23);            // (255: the conversion gives no numbers)
-        const uint32_t at = v_put + buf * GEO::V_BYTES;
+        const uint32_t at = put_at + buffer;
         unsigned char *even = smem + (at + turn * 16), *odd = smem + (at + 16 - turn * 16);
 #pragma unroll
         for (int w = 0; w < LW; w += 2) {
@@ -270,11 +254,12 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
             *reinterpret_cast<uint4 *>(odd + w * 16) = widen_word<T>(c, scale);
         }
     };
-    // V of stage s is put while stage s - 1 is computed, K while stage s - 2 is, whose last step forms the first scores of stage s - 1; both are asked
-    // for a stage before that.
+    // V of stage s is put while stage s - 1 is computed, and so is K, but that the pages of a key group's first step are those of stage s + 1: the last step
+    // of a stage forms the first scores of the next.  Both are asked for a stage before that.
     constexpr bool kPipe = TPW <= 2;                 // (three tiles leave no registers for two generations of scores)
-    Held k_held = load(p.k, p.k_scale, 0), v_held = load(p.v, p.v_scale, 0), k_next{};
-    if constexpr (kPipe) k_next = load(p.k, p.k_scale, 1);
+    const int early = kPipe && wave % (2 * STEPS) < 2 ? 1 : 0;
+    Held k_held = load(p.k, p.k_scale, early), v_held = load(p.v, p.v_scale, 0), k_first{};
+    if constexpr (kPipe) k_first = load(p.k, p.k_scale, 0);
 
     // ---- query rows: tiles wr, wr + WR, ... of the row group ----
     const float inv_g = __builtin_amdgcn_rcpf((float)p.G);
@@ -288,7 +273,7 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
         const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        q[t] = load_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
+        q[t] = load_query<T, D, false>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
         take_query(q[t], irow[t] >= 0, p.c_log2);
     }
     const int my_tiles = max(0, (min(p.group_tiles, p.RT - rg * p.group_tiles) - wr + WR - 1) / WR);       // wave-uniform
@@ -305,38 +290,14 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     }
 
     // ---- one step of 32 tokens ----
-    const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * GEO::KROW + (D == 128 ? GEO::k_piece(j, qd) * 16 : GEO::k_piece(j, qd >> 1) * 16 + (qd & 1) * 8);
-    const uint32_t ks_take = GEO::K + GEO::K_BYTES + (j * NG + (D == 128 ? qd : qd >> 1)) * 8;
-    const uint32_t v_take = (wk * STEPS * 32 + 4 * qd + (j >> 2)) * kVRow<D> + (j & 3) * 8;
-    struct Codes {
-        uint32_t key[2][LW];                         // of 16 keys each
-    };
-    auto load_codes = [&](const unsigned char *k_rows) -> Codes {
-        typedef typename std::conditional<LW == 4, Words4, Words2>::type Words;
-        Codes c;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const Words x = *reinterpret_cast<const Words *>(k_rows + kt * kPage * GEO::KROW);
-#pragma unroll
-            for (int w = 0; w < LW; ++w) c.key[kt][w] = x[w];
-        }
-        return c;
+    const uint32_t k_take = GEO::K + (wk * STEPS * 32 + j) * kRow<D> + qd * 16;
+    const uint32_t v_take = (wk * STEPS * 32 + 4 * qd + (j >> 2)) * kRow<D> + (j & 3) * 8;
+    auto load_k_frag = [&](const unsigned char *k_rows, int kt, int w) -> uint4 {
+        return *reinterpret_cast<const uint4 *>(k_rows + kt * kPage * kRow<D> + w * 64);
     };
     auto load_v_frag = [&](const unsigned char *v_rows, int u) -> uint4 {
-        const uint2 lo = lds_read_tr16(v_rows + u * 32), hi = lds_read_tr16(v_rows + u * 32 + kPage * kVRow<D>);
+        const uint2 lo = lds_read_tr16(v_rows + u * 32), hi = lds_read_tr16(v_rows + u * 32 + kPage * kRow<D>);
         return make_uint4(lo.x, lo.y, hi.x, hi.y);
-    };
-    // the word that holds scale bytes 2 i and 2 i + 1 of this key group: of the two all (WK 1), one (2), or half of one (4)
-    auto scale_word = [&](auto i_tag, uint2 words) -> uint32_t {
-        uint32_t word = WK == 1 ? (decltype(i_tag)::value < 2 ? words.x : words.y) : (wk >= WK / 2 ? words.y : words.x);
-        if (WK == 4) word >>= 16 * (wk & 1);
-        return word;
-    };
-    auto scores = [&](auto i_tag, auto na_tag, const Codes &codes, uint2 words, f32x4 (&s)[TPW][2]) {
-        constexpr int i = decltype(i_tag)::value, NA = decltype(na_tag)::value;
-        const uint32_t word = scale_word(i_tag, words);
-        score<T, D, NA>(codes.key[0], scale_of<(2 * i) & 3>(word), q, 0, s);
-        score<T, D, NA>(codes.key[1], scale_of<(2 * i + 1) & 3>(word), q, 1, s);
     };
     auto mask = [&](f32x4 (&s)[2], int t, int step_pos) {
         const int node = max(irow[t], 0);
@@ -380,16 +341,16 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     };
     const uint4 ones = make_uint4(ones2<T>(), ones2<T>(), ones2<T>(), ones2<T>());
 
-    // Up to two tiles a wavefront.  S, the step's scores, are there already; V's fragments and the next step's codes are asked for before the softmax, and the products
-    // that form the next scores run in one burst with those of the values, 34 of them, while the SIMD's other wavefront has its softmax.  A score above its row's room shows when the weights are formed, which are then
-    // formed again.
-    auto piped_step = [&](auto na_tag, f32x4 (&S)[TPW][2], f32x4 (&next)[TPW][2], const unsigned char *next_codes, auto next_tag, uint2 next_words,
-                          const unsigned char *v_rows, int step_pos) {
+    // Up to two tiles a wavefront.  S, the step's scores, are there already; the next step's keys are asked for first and multiplied before the weights are
+    // formed, and V's fragments, in the same registers, behind those products.  (Half of V's, or the next keys, asked for earlier: no registers, 49-57 us for
+    // 104 rows over 64K.)  A score above its row's room shows when the weights are formed, which are then formed again.
+    auto piped_step = [&](auto na_tag, f32x4 (&S)[TPW][2], f32x4 (&next)[TPW][2], const unsigned char *next_rows, const unsigned char *v_rows, int step_pos) {
         constexpr int NA = decltype(na_tag)::value;
-        uint4 vf[NT], pf[TPW];
-        const Codes codes = load_codes(next_codes);
+        uint4 vf[NT], pf[TPW], kf[2][LW];
 #pragma unroll
-        for (int u = 0; u < NT; ++u) vf[u] = load_v_frag(v_rows, u);
+        for (int w = 0; w < LW; ++w)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) kf[kt][w] = load_k_frag(next_rows, kt, w);
         asm volatile("" ::: "memory");               // (no load sinks below)
         if (step_pos + 32 > L)                       // reaches drafts or the ragged end (uniform)
 #pragma unroll
@@ -400,7 +361,15 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
             exponents(S[t], t, x[t]);
             top = fmaxf(top, highest(x[t]));
         }
-        scores(next_tag, na_tag, codes, next_words, next);
+#pragma unroll
+        for (int w = 0; w < LW; ++w)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int t = 0; t < NA; ++t) next[t][kt] = mfma16<T>(kf[kt][w], q[t].part[w], w == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : next[t][kt]);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int u = 0; u < NT; ++u) vf[u] = load_v_frag(v_rows, u);
 #pragma unroll
         for (int t = 0; t < NA; ++t) pf[t] = weights(x[t]);
         if (__builtin_amdgcn_ballot_w64(top > kGroupRoom<T>) != 0) {             // any lane's own keys can raise the alarm (uniform, rarely taken after the first step)
@@ -420,15 +389,21 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     };
     // Three tiles: registers for one generation of scores, all of a step's ahead of the softmax, and for a few of V's fragments.
     constexpr int kAhead = 3;
-    auto plain_step = [&](auto i_tag, auto na_tag, const unsigned char *k_rows, uint2 words, const unsigned char *v_rows, int step_pos) {
+    auto plain_step = [&](auto na_tag, const unsigned char *k_rows, const unsigned char *v_rows, int step_pos) {
         constexpr int NA = decltype(na_tag)::value;
         uint4 vf[NT], pf[TPW];
-        const Codes codes = load_codes(k_rows);
+        f32x4 s[TPW][2];
+#pragma unroll
+        for (int w = 0; w < LW; ++w)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const uint4 kf = load_k_frag(k_rows, kt, w);
+#pragma unroll
+                for (int t = 0; t < NA; ++t) s[t][kt] = mfma16<T>(kf, q[t].part[w], w == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][kt]);
+            }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) vf[u] = load_v_frag(v_rows, u);
         asm volatile("" ::: "memory");
-        f32x4 s[TPW][2];
-        scores(i_tag, na_tag, codes, words, s);
 #pragma unroll
         for (int t = 0; t < NA; ++t) {
             if (step_pos + 32 > L) mask(s[t], t, step_pos);
@@ -452,70 +427,57 @@ __device__ __forceinline__ void run_group_piece(const QuantParams &p, unsigned c
     };
 
     // ---- the loop ----
-    put_k(k_held, 0);
-    put_v(v_held, 0);
+    put(k_held, GEO::K);
+    put(v_held, 0);
     v_held = load(p.v, p.v_scale, 1);
-    k_held = load(p.k, p.k_scale, kPipe ? 2 : 1);
-    if constexpr (kPipe) put_k(k_next, GEO::K_STAGE);
+    k_held = load(p.k, p.k_scale, 1 + early);
+    if constexpr (kPipe) put(k_first, GEO::K + GEO::T_BYTES);
     __syncthreads();
     auto run = [&](auto na_tag) {
         constexpr int NA = decltype(na_tag)::value;
-        using First = std::integral_constant<int, 0>;
         f32x4 Sa[TPW][2], Sb[TPW][2];
-        uint2 words{};
-        if constexpr (kPipe && NA > 0) {
-            words = *reinterpret_cast<const uint2 *>(smem + ks_take);
-            scores(First{}, na_tag, load_codes(smem + k_take), words, Sa);
-        }
-        uint32_t ring = 0;                           // of K
-        for (int s = 0; s < stages; ++s) {
-            const int buf = s & 1;
-            const uint32_t ring1 = ring == 2 * GEO::K_STAGE ? 0 : ring + GEO::K_STAGE, ring2 = ring1 == 2 * GEO::K_STAGE ? 0 : ring1 + GEO::K_STAGE;
-            put_v(v_held, buf ^ 1);
-            if constexpr (kPipe) {
-                v_held = load(p.v, p.v_scale, s + 2);
-                put_k(k_held, ring2);
-                if (((s + 3) & 63) == 0 && s + 3 < stages) pages = stage_pages(s + 3);
-                k_held = load(p.k, p.k_scale, s + 3);
-            } else {
-                put_k(k_held, ring1);
-                if (((s + 2) & 63) == 0 && s + 2 < stages) pages = stage_pages(s + 2);
-                v_held = load(p.v, p.v_scale, s + 2);
-                k_held = load(p.k, p.k_scale, s + 2);
-            }
+        if constexpr (kPipe) {
             if constexpr (NA > 0) {
-                const unsigned char *k_rows = smem + (k_take + ring), *k_rows1 = smem + (k_take + ring1), *v_rows = smem + (v_take + buf * GEO::V_BYTES);
-                const int pos = pos0 + s * kStage + wk * STEPS * 32;
-                if constexpr (kPipe) {
-                    const uint2 words1 = *reinterpret_cast<const uint2 *>(smem + (ks_take + ring1));
-                    static_for<0, STEPS>([&](auto i_tag) {
-                        constexpr int i = decltype(i_tag)::value;
-                        if (pos + i * 32 >= pos1) return;                        // uniform
-                        f32x4 (&now)[TPW][2] = i % 2 ? Sb : Sa, (&then)[TPW][2] = i % 2 ? Sa : Sb;
-                        // (the last step forms scores of what lies behind the end, for nobody)
-                        if constexpr (i + 1 < STEPS)
-                            piped_step(na_tag, now, then, k_rows + (i + 1) * 32 * GEO::KROW, std::integral_constant<int, i + 1>{}, words,
-                                       v_rows + i * 32 * kVRow<D>, pos + i * 32);
-                        else
-                            piped_step(na_tag, now, then, k_rows1, First{}, words1, v_rows + i * 32 * kVRow<D>, pos + i * 32);
-                    });
-                    words = words1;
-                    if constexpr (STEPS % 2 == 1)
 #pragma unroll
-                        for (int t = 0; t < NA; ++t) {
-                            Sa[t][0] = Sb[t][0];
-                            Sa[t][1] = Sb[t][1];
-                        }
-                } else {
-                    words = *reinterpret_cast<const uint2 *>(smem + (ks_take + ring));
-                    static_for<0, STEPS>([&](auto i_tag) {
-                        constexpr int i = decltype(i_tag)::value;
-                        if (pos + i * 32 < pos1)
-                            plain_step(i_tag, na_tag, k_rows + i * 32 * GEO::KROW, words, v_rows + i * 32 * kVRow<D>, pos + i * 32);     // uniform
-                    });
-                }
+                for (int w = 0; w < LW; ++w)
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt) {
+                        const uint4 kf = load_k_frag(smem + (k_take + GEO::T_BYTES), kt, w);
+#pragma unroll
+                        for (int t = 0; t < NA; ++t) Sa[t][kt] = mfma16<T>(kf, q[t].part[w], w == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : Sa[t][kt]);
+                    }
             }
-            ring = ring1;
+            __syncthreads();
+        }
+        for (int s = 0; s < stages; ++s) {
+            const uint32_t now = s & 1 ? GEO::T_BYTES : 0, then = GEO::T_BYTES - now;
+            put(v_held, then);
+            if (!early && ((s + 2) & 63) == 0 && s + 2 < stages) pages = stage_pages(s + 2);
+            v_held = load(p.v, p.v_scale, s + 2);
+            put(k_held, GEO::K + then);
+            if (early && ((s + 3) & 63) == 0 && s + 3 < stages) pages = stage_pages(s + 3);
+            k_held = load(p.k, p.k_scale, s + 2 + early);
+            if constexpr (NA > 0) {
+                const unsigned char *k_rows = smem + (k_take + now), *v_rows = smem + (v_take + now);
+                const int pos = pos0 + s * kStage + wk * STEPS * 32;
+                static_for<0, STEPS>([&](auto i_tag) {
+                    constexpr int i = decltype(i_tag)::value;
+                    if (pos + i * 32 >= pos1) return;                            // uniform
+                    if constexpr (kPipe) {
+                        f32x4 (&S)[TPW][2] = i % 2 ? Sb : Sa, (&next)[TPW][2] = i % 2 ? Sa : Sb;
+                        // (the last step forms scores of what lies behind the end, for nobody)
+                        piped_step(na_tag, S, next, k_rows + (i + 1) % STEPS * 32 * kRow<D>, v_rows + i * 32 * kRow<D>, pos + i * 32);
+                    } else {
+                        plain_step(na_tag, k_rows + i * 32 * kRow<D>, v_rows + i * 32 * kRow<D>, pos + i * 32);
+                    }
+                });
+                if constexpr (kPipe && STEPS % 2 == 1)
+#pragma unroll
+                    for (int t = 0; t < NA; ++t) {
+                        Sa[t][0] = Sb[t][0];
+                        Sa[t][1] = Sb[t][1];
+                    }
+            }
             __syncthreads();
         }
     };
@@ -643,7 +605,7 @@ __global__ void __launch_bounds__(kThreads) splitkv_groups_kernel(const QuantPar
 // ---------------------------------------------------------------------------
 template <int D>
 struct OGeo {
-    static constexpr int NT = D / 16, NG = D / 32, VROW = kVRow<D>, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
+    static constexpr int NT = D / 16, NG = D / 32, VROW = kRow<D>, LW = D / 32;    // LW: words of K and of V that a lane brings from a page
     static constexpr int CHUNK = 2 * kPage, WAVE = CHUNK * VROW;
     static constexpr int DEPTH = 2;                              // chunks under way
     static constexpr int TILE = NT * 1024 + 512;
@@ -684,7 +646,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
         const int row = tg * kRowTile + j, i = (int)(((float)row + 0.5f) * inv_g);     // node row / G, exactly (see owl_splitkv.h)
         irow[t] = tile_ok && row < p.R && i < Nb ? i : -1;
         const int rc = min(row, p.R - 1), ic = (int)(((float)rc + 0.5f) * inv_g);
-        q[t] = load_query<T, D>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
+        q[t] = load_query<T, D, true>(q_head + ((int64_t)ic * (p.Hq - p.G) + rc) * (D * 2), qd);
     }
 
     // Bad pages are page 0; behind the piece's end it is the piece's last one.
@@ -744,7 +706,7 @@ __device__ __forceinline__ void run_own_piece(const QuantParams &p, unsigned cha
     auto step = [&](Held &h, int i, auto more_tag) {
         f32x4 S[TPW][2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) score<T, D, TPW>(h.k[kt], __builtin_bit_cast(float, h.ks[kt] << 23), q, kt, S);
+        for (int kt = 0; kt < 2; ++kt) score<T, D>(h.k[kt], __builtin_bit_cast(float, h.ks[kt] << 23), q, kt, S);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const float scale = __builtin_bit_cast(float, h.vs[kt] << 23);           // (255: the conversion gives no numbers)
