@@ -87,25 +87,29 @@ owl_status check_quant_desc(const owl_verify_desc *d, Cached cached = Cached::kB
 // The row tiles of a workgroup over 4-bit groups, and how its wavefronts share the work (owl_splitkv_groups.hip).
 void plan_groups(const owl_verify_desc *d, int RT, int64_t T, int64_t cmin, int *tpw, int *wr, int *wk, int *rgs, int *group_tiles)
 {
-    // Three ways.  us of a lone sequence of 8 KV heads, 4 query heads each, with 2-tile groups over shared stages / keys of a wavefront's own / groups
+    // Three ways.  us of a lone sequence of 8 KV heads, 4 query heads each, bf16, with 2-tile groups over shared stages / keys of a wavefront's own / groups
     // of many tiles over shared stages:
-    //    2 tiles   1K 10.0 / 11.5     5K 11.4 / 12.5    16K 14.8 / 14.7    32K 19.4 / 17.9   128K 43.0 / 33.9
-    //    4 tiles   1K 10.6 / 11.7 / 13.9    5K 12.7 / 13.6 / 15.6    10K - / 15.9 / 17.6    64K - / 32.5 / 33.4   128K - / 52.5 / 51.5
-    //    8 tiles   1K 11.0 / 12.3 / 15.1    10K - / 18.5 / 20.1    16K - / 21.9 / 21.1     32K - / 32.4 / 29.3
-    //   15 tiles   1K 12.5 / 13.5 / 16.6    2K 14.4 / 15.0 / 16.9    10K - / 24.8 / 27.1   16K - / 32.0 / 28.2
-    // The first has little to set up, the second streams the cache, the third reads it least often.  Batches: 2 tiles, 16 of 5K 35.8 / 32.1, 16 of
-    // 8K-64K 180 / 136; 4 tiles, 16 of 5K - / 46.5 / 39.6, 16 of 8K-64K - / 242 / 226.
+    //    2 tiles   1K 10.0 / 10.5     3K 10.7 / 10.8     5K 11.7 / 11.3    16K 15.1 / 14.0    32K 21.0 / 18.5   128K 53 / 39
+    //    4 tiles   1K 10.6 / 10.8 / 13.3     3K 11.4 / 11.5 / 14.5     5K 12.8 / 12.4 / 15.3    16K 19.4 / 16.5 / 19.4    128K - / 58.3 / 60.0    256K - / 110.0 / 109.8
+    //    8 tiles   1K 11.0 / 11.2 / 14.2     2K 12.2 / 11.6 / 14.5    10K 21.7 / 17.5 / 20.6    20K - / 23.8 / 24.1    32K - / 32.3 / 31.7
+    //   15 tiles   1K 12.6 / 12.3 / 16.0     5K 22.1 / 18.1 / 20.9    10K - / 24.4 / 28.7     12K - / 26.9 / 26.1    16K - / 31.7 / 30.1
+    // The first has little to set up, the second streams the cache, the third reads it least often.  fp16 is within 1 us of that; head_dim 64 has the same borders: 2
+    // tiles 5K 9.0 / 9.4, 10K 10.9 / 10.0, 4 tiles 5K 10.2 / 9.9, 64K - / 24.8 / 27.3, 8 tiles 16K - / 16.2 / 16.4, 32K - / 23.4 / 21.9, 15 tiles 10K - / 18.1 / 21.3,
+    // 16K - / 23.3 / 21.8.  Batches, the second / the third: 2 tiles, 16 of 5K 32 / 41, of 8K-64K 155 / 233; 4 tiles, 16 of 2K 25.5 / 32.8, of 5K 42.2 / 49.3,
+    // 64 of 100-2000 71.5 / 62.7, 16 of 8K-64K 273 / 269; 5 tiles, 16 of 120 22.2 / 17.4, of 5K 68 / 59; 8 tiles, 4 of 500 14.6 / 16.7, of 2K 18.6 / 20.5, of 5K 29.6 / 26.4;
+    // 15 tiles, 4 of 2K 24.0 / 25.9, of 5K 40 / 34.
     const int pairs = (RT + 1) / 2;
     const int64_t tokens = d->batch * T * d->n_kv_heads / device_cus();          // of a compute unit, where every row is its own
-    const bool brief = RT > 1 && RT <= 16 && tokens * pairs <= 512, lone = d->batch == 1 && RT <= 16 && tokens <= (RT <= 4 ? 2560 : 384);
-    if (!brief && (pairs == 1 || lone)) {            // keys of a wavefront's own
+    const bool brief = RT > 1 && RT <= 16 && tokens * pairs <= 128 && (RT <= 4 || d->batch <= 4);
+    const int64_t most_own = RT <= 4 ? (d->batch == 1 ? 4096 : 2560) : RT > 16 || d->batch > 4 ? 0 : d->batch > 1 ? 256 : RT <= 8 ? 768 : 384;
+    if (!brief && (pairs == 1 || tokens <= most_own)) {      // keys of a wavefront's own
         *rgs = pairs;
         *group_tiles = *tpw = (RT + pairs - 1) / pairs;
         *wr = pairs > 1 ? 2 : 1;
         *wk = kWavesPerGroup;
         return;
     }
-    // As many tiles as the wavefronts' registers hold (three parts of an fp16 query take more), and fewer until the groups times the splits of cmin
+    // As many tiles as the wavefronts hold in registers (24; fp16 has no kernel of three tiles a wavefront), and fewer until the groups times the splits of cmin
     // tokens fill three quarters of the compute units.
     const int most = brief ? 2 : d->qkv_dtype == OWL_F16 ? 16 : 24;
     int n = (RT + most - 1) / most;

@@ -60,7 +60,7 @@ def _check(gc, step, what):
 SPLITS = {
     "own keys, 1 tile": (4, 4, 2, None, True, (1, 1), (1, 1)), "own keys, 2 tiles": (8, 4, 1, 1 << 18, True, (2, 1), (2, 1)),
     "own keys, 2 groups": (16, 4, 1, 1 << 17, True, (2, 2), (2, 2)), "own keys, 8 groups": (60, 4, 1, None, True, (2, 8), (2, 8)),
-    "shared, groups of 2 tiles": (12, 4, 1, None, False, (1, 2), (1, 2)), "shared, 3 tiles in all": (12, 4, 1, 1 << 22, False, (2, 1), (2, 1)),
+    "shared, 2 tiles in all": (8, 4, 1, None, False, (1, 1), (1, 1)), "shared, 3 tiles in all": (12, 4, 1, 1 << 22, False, (2, 1), (2, 1)),
     "shared, 4 tiles": (16, 4, 1, 1 << 22, False, (2, 1), (2, 1)), "shared, 7 tiles": (28, 4, 1, 1 << 22, False, (2, 1), (2, 1)),
     "shared, 15 tiles": (60, 4, 1, 1 << 22, False, (2, 1), (2, 1)), "shared, 20 tiles": (40, 8, 1, 1 << 22, False, (3, 1), (2, 2)),
 }
