@@ -312,11 +312,12 @@ __device__ __forceinline__ void store_groups(const Piece<T> &a, const Piece<T> &
 // ---------------------------------------------------------------------------
 // Append to a cache in the rows' own type, or (kFour) of 4-bit groups, which ask nothing of other tokens either: one workgroup per
 // token, an item a thread.  kNorm: with the norms of the heads.
-// Many tokens are bound by memory: a prompt of 8K in fp16, 201 MB, 45 us with the norms and 40 without (4.4 and 5.0 TB/s); four chunks of 2501
-// into 4 bits, 380 MB, 74 us (5.1 TB/s).  Few are bound by a workgroup's chain, lengths -> page, angles and products in 64 bits, of which an
-// item with the norm has some 200: with 384 threads, which 48 heads of 128 channels are in one pass, a tree of 60 tokens takes 4.5 us
-// and 16 trees of up to 26 into 4 bits 6.4; with 256 5.3 and 6.9, but of 1024 tokens 8.7 and 9.1 us, of 2048 14.8 and 13.6, of 8192 53 and 45.  (With the rows asked for before
-// the lengths, 5.5 and 7.0: they wait for nothing that the angles do not take as long as.)
+// Many tokens are bound by memory: a prompt of 8K in fp16, 201 MB, 43 us with the norms and 40 without (4.7 and 5.0 TB/s), in fp32 78 (5.2 TB/s), with the norms into 4 bits
+// 45 (3.9); four chunks of 2501 into 4 bits, 380 MB, 75 us (5.1 TB/s).  Few are bound by a workgroup's chain, lengths -> page, angles and products in 64 bits, of which an
+// item with the norm has some 200: with 384 threads, which 48 heads of 128 channels are in one pass, a tree of 60 tokens takes 4.3 us
+// and 16 trees of up to 26 into 4 bits 6.3; with 256 5.2 and 6.9.  Where 256 threads take more than one pass, 384 / 256, us, of 700, 1024 and 2048 tokens: 48 heads 7.4 / 7.7, 8.6 / 9.1,
+// 14.4 / 13.4, into 4 bits 7.6 / 8.1, 9.9 / 9.5, 16.3 / 14.3; 80 heads 10.1 / 10.6, 12.3 / 12.2, 23.4 / 22.1; fp32, 48 heads, 8.2 / 8.4, 10.6 / 10.4, 22.6 / 23.1.  Where they take one, 18 heads,
+// 4.0 / 3.9 of 60, 5.5 / 5.2 of 700.  (With the rows asked for before the lengths, 5.5 and 7.0: they wait for nothing that the angles do not take as long as.)
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256, kNormThreads = 384, kNormTokens = 768;
 
@@ -593,8 +594,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_quant_kernel(const Appe
 template <typename T, int D, bool kPairs, bool kNorm, bool kFour>
 static void launch_append_tokens(const AppendArgs &p, int B, hipStream_t s)
 {
+    const int64_t items = ((int64_t)(p.q ? p.Hq : 0) + 2 * (int64_t)p.Hkv) * (D / (2 * Piece<T>::E));
     if constexpr (kNorm)
-        if ((int64_t)p.n * B <= kNormTokens) {
+        if (items > kAppendThreads && (int64_t)p.n * B <= kNormTokens) {
             hipLaunchKernelGGL((append_kernel<T, D, kPairs, kNorm, kFour, kNormThreads>), dim3(p.n, B), dim3(kNormThreads), 0, s, p);
             return;
         }

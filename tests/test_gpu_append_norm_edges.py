@@ -1,5 +1,5 @@
-"""Rows with an infinite number or none on their way into caches of 4-bit groups: which scale bytes say so, with and without the norms of the heads.  Needs
-an MI355X (-m gpu)."""
+"""Appending with the norms of the heads: rows with an infinite number or none on their way into caches of 4-bit groups, and heads and tokens about the numbers at
+which the launch changes.  Needs an MI355X (-m gpu)."""
 import numpy as np
 import pytest
 import torch
@@ -41,3 +41,29 @@ def test_which_groups_are_none(dtype, norm, pairs):
             if norm and i in (0, 2, 3):
                 assert all(k[h, g] == least for g in range(4) if g not in want), (i, h)
     a.check()
+
+
+def _check_fp32(a, q):
+    """Both sides work in 64 bits, in another order: they are apart by some 2^-51 of the greater of the two terms x cos, y sin whose difference is taken.  Where that
+    moves a number over a tie of fp32 the two round to neighbours, one step of at most 2^-23 apart; for N numbers, terms k times greater than their
+    difference, that is N 2 2^-51 k / 2^-23 of them, 0.02 k of 2.75 M, and k is some ten on average (one number of 36 times smaller than its terms lies 1.0e-15 from a tie)."""
+    torch.cuda.synchronize()
+    wq, wk, wv = a.want()
+    pairs = [(d.cpu().numpy().reshape(w.shape), w) for d, w in zip(a.dev[:2], (wk, wv))]
+    if q:
+        pairs.append((a.q_out.cpu().numpy(), wq))
+    for got, want in pairs:
+        assert (np.abs(got.astype(np.float64) - want) <= 2.0 ** -23 * np.abs(want)).all() and np.sum(got != want) <= 4, np.sum(got != want)
+
+
+@pytest.mark.parametrize("dtype,cache", [(W.DT_BF16, "own"), (W.DT_F16, "own"), (W.DT_F32, "own"), (W.DT_BF16, "groups"), (W.DT_F16, "groups")])
+@pytest.mark.parametrize("Hq,Hkv,n,q", [(24, 4, 768, True), (28, 4, 768, True), (28, 4, 769, True), (24, 4, 769, True), (28, 4, 700, False), (16, 16, 5, True), (16, 16, 5, False)])
+def test_heads_and_tokens_about_the_borders(dtype, cache, Hq, Hkv, n, q):
+    """32 heads of 128 channels in 16 bits are one item a thread of 256 threads, 36 are more; without queries fewer."""
+    a = Rows(n + Hq, dtype=dtype, cache=cache, norm=True, Hq=Hq, Hkv=Hkv, D=128, ctx=[5], n=n, rot_dim=128)
+    a.run(q=q)
+    if dtype == W.DT_F32:
+        _check_fp32(a, q)
+    else:
+        a.check(q=q)
+    assert int(a.status.item()) == 0
