@@ -15,10 +15,10 @@
 // The wavefronts are WR row groups of TPW tiles times WK key groups, which take the 32-token steps of a stage in turn and merge at the end of a piece.
 // Keys of a wavefront's own, for few rows: further below.
 //
-// What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 120 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes
-// and scales); products, fragments from LDS and softmax beside each other where rows are many, 162 us for 320 rows over 128K in bf16 (1.06 PFLOP/s; fp16, in
-// two row groups, 195).  Between the two, 104 rows at 64K 47 us, in 16 sequences 365 (fp16 370): 16 KB of fragments from LDS take as long as the 34 products
-// that two tiles make of them.
+// What bounds it (8 KV heads, head_dim 128): the stream for a row or two, 120-123 us for 16 sequences of 8K-64K at one node each (6.0 TB/s of codes and
+// scales); products, fragments from LDS and softmax beside each other where rows are many, 161 us for 320 rows over 128K in bf16 (1.07 PFLOP/s; fp16, in two row
+// groups, 195).  Between the two, 104 rows at 64K 47 us, in 16 sequences 362 (fp16 367): by counters the matrix pipe is busy for 38 % of the time and LDS for 31 %, a
+// wavefront issues for 35 % of its cycles, is ready without issuing for 31 % (its SIMD's pipe or other wavefront) and waits for 33 % (barrier, LDS, memory).
 #include "owl_splitkv.h"
 
 namespace owl {
